@@ -90,6 +90,8 @@ typedef enum {
  * the workspace is sized for the forward pass alone (no dZ scratch, no dW sums); the entry points
  * that compute gradients return ALST_ERR_UNSUPPORTED for it. */
 #define ALST_FLAG_FORWARD_ONLY 16u
+/* The rows of a residual stream are fp32 instead of bf16 (alst_embedding.h, alst_block_norm.h; refused elsewhere). */
+#define ALST_FLAG_RESIDUAL_FP32 32u
 
 /* Static, NUL-terminated description of a status value.  Host only. */
 const char* alst_status_string(int status);

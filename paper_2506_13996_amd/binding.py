@@ -23,6 +23,7 @@ ALST_FLAG_DW_ACCUMULATE = 2
 ALST_FLAG_REDUCE_SUM = 4
 ALST_FLAG_TILE_SCRATCH = 8
 ALST_FLAG_FORWARD_ONLY = 16
+ALST_FLAG_RESIDUAL_FP32 = 32
 
 EXPORTS = (
     "alst_status_string", "alst_version", "alst_tiled_ce_workspace_bytes", "alst_tiled_ce_forward",
@@ -33,6 +34,12 @@ EXPORTS = (
     "alst_debug_layer", "alst_debug_ce_chunk", "alst_debug_mfma_rate",
     "alst_tiled_mlp_workspace_bytes", "alst_tiled_mlp_forward", "alst_tiled_mlp_backward",
     "alst_tiled_linear_workspace_bytes", "alst_tiled_linear_forward", "alst_tiled_linear_backward",
+)
+# the operators around the tiled layers (alst_embedding.h, alst_block_norm.h, alst_grads.h)
+STEP_EXPORTS = (
+    "alst_embedding_workspace_bytes", "alst_embedding_forward", "alst_embedding_backward",
+    "alst_block_norm_workspace_bytes", "alst_block_norm_forward", "alst_block_norm_backward",
+    "alst_grad_norm_workspace_bytes", "alst_grad_norm", "alst_grad_clip", "alst_grad_norm_clip",
 )
 
 
@@ -50,6 +57,12 @@ class LayerInfo(ctypes.Structure):
     _fields_ = [("rows", ctypes.c_int64)] + \
                [(n, ctypes.c_int) for n in ("transposed", "gated_columns", "gated_chained", "product_columns",
                                             "product_chained", "wgrad_columns", "together")]
+
+
+class GradTensor(ctypes.Structure):
+    """alst_grad_tensor (alst_grads.h)."""
+    _fields_ = [("grad", ctypes.c_void_p), ("out", ctypes.c_void_p), ("n", ctypes.c_int64), ("fp32", ctypes.c_int32),
+                ("reserved", ctypes.c_int32)]
 
 
 _lib = None
@@ -105,6 +118,28 @@ def load_library() -> ctypes.CDLL:
     lib.alst_tiled_linear_forward.argtypes = [vp, vp, i64, i64, i64, i64, vp, vp, sz, u32, vp]
     lib.alst_tiled_linear_backward.restype = c.c_int
     lib.alst_tiled_linear_backward.argtypes = [vp, vp, vp, i64, i64, i64, i64, vp, vp, vp, sz, u32, vp]
+    lib.alst_embedding_workspace_bytes.restype = sz
+    lib.alst_embedding_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.alst_embedding_forward.restype = c.c_int
+    lib.alst_embedding_forward.argtypes = [vp, vp, i64, i64, i64, i32, f32, vp, vp, u32, vp]
+    lib.alst_embedding_backward.restype = c.c_int
+    lib.alst_embedding_backward.argtypes = [vp, vp, i64, i64, i64, i32, f32, vp, vp, sz, u32, vp]
+    lib.alst_block_norm_workspace_bytes.restype = sz
+    lib.alst_block_norm_workspace_bytes.argtypes = [i64, i64]
+    lib.alst_block_norm_forward.restype = c.c_int
+    lib.alst_block_norm_forward.argtypes = [vp, vp, vp, vp, i64, vp, i64, i64, f32, f32, f32, vp, vp, u32, vp]
+    lib.alst_block_norm_backward.restype = c.c_int
+    lib.alst_block_norm_backward.argtypes = [vp, vp, vp, vp, i64, vp, vp, vp, i64, i64, f32, f32, f32, vp, vp, vp, vp, vp,
+                                             vp, sz, u32, vp]
+    tensors = c.POINTER(GradTensor)
+    lib.alst_grad_norm_workspace_bytes.restype = sz
+    lib.alst_grad_norm_workspace_bytes.argtypes = [i64]
+    lib.alst_grad_norm.restype = c.c_int
+    lib.alst_grad_norm.argtypes = [tensors, i64, vp, vp, vp, sz, vp]
+    lib.alst_grad_clip.restype = c.c_int
+    lib.alst_grad_clip.argtypes = [tensors, i64, vp, f32, vp, vp]
+    lib.alst_grad_norm_clip.restype = c.c_int
+    lib.alst_grad_norm_clip.argtypes = [tensors, i64, f32, vp, vp, vp, sz, vp]
     lib.alst_profile_enable.restype = c.c_int
     lib.alst_profile_enable.argtypes = [c.c_int]
     lib.alst_profile_read.restype = c.c_int
@@ -376,6 +411,209 @@ def alst_tiled_linear_backward(x, W, dy, tile: int, *, dx, dW, workspace, flags:
                                                    0 if workspace is None else workspace.numel(),
                                                    flags, _stream())
     _check(st, "alst_tiled_linear_backward")
+
+
+def _call(where: str, tensors: dict, *args) -> None:
+    """Calls an entry point on the current stream of the device that all `tensors` are on (and only there: another
+    device may be the current one).  The last check of a wrapper, like _on_device."""
+    _on_device(**tensors)
+    devices = {t.device for t in tensors.values() if t is not None}
+    if len(devices) != 1:
+        raise TypeError(f"{where}: tensors on different devices: {sorted(str(d) for d in devices)}")
+    with torch.cuda.device(devices.pop()):
+        st = getattr(load_library(), where)(*args, _stream())
+    _check(st, where)
+
+
+def _rows_type(flags: int):
+    return torch.float32 if flags & ALST_FLAG_RESIDUAL_FP32 else torch.bfloat16
+
+
+def alst_embedding_workspace_bytes(N: int, H: int, V: int) -> int:
+    return int(load_library().alst_embedding_workspace_bytes(N, H, V))
+
+
+def alloc_embedding_workspace(N: int, H: int, V: int, device="cuda") -> torch.Tensor:
+    nbytes = alst_embedding_workspace_bytes(N, H, V)
+    if nbytes == 0:
+        raise AlstError(ALST_ERR_SHAPE, "alst_embedding_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _want_2d(t, name: str, dtype):
+    _want(t, name, dtype)
+    if t.dim() != 2:
+        raise TypeError(f"{name}: expected two dimensions, got shape {tuple(t.shape)}")
+    return t.shape
+
+
+def alst_embedding_forward(tokens, E, scale: float = 1.0, ignore_index: int = -100, *, y, device_status_out=None,
+                           flags: int = 0) -> None:
+    """y [N,H] = scale * E[tokens]; tokens [N] int32, E [V,H] bf16, y bf16 (fp32 with ALST_FLAG_RESIDUAL_FP32)."""
+    V, H = _want_2d(E, "E", torch.bfloat16)
+    N, _ = _want_2d(y, "y", _rows_type(flags))
+    _want(tokens, "tokens", torch.int32, (N,))
+    _want(y, "y", _rows_type(flags), (N, H))
+    _want(device_status_out, "device_status_out", torch.int32, (1,), optional=True)
+    _call("alst_embedding_forward", dict(tokens=tokens, E=E, y=y, device_status_out=device_status_out),
+          _ptr(tokens), _ptr(E), N, H, V, ignore_index, scale, _ptr(y), _ptr(device_status_out), flags)
+
+
+def alst_embedding_backward(tokens, dy, scale: float = 1.0, ignore_index: int = -100, *, dE, workspace,
+                            flags: int = 0) -> None:
+    """dE [V,H] = scale * the sum of each token's rows of dy [N,H] (+= with ALST_FLAG_DW_ACCUMULATE)."""
+    N, H = _want_2d(dy, "dy", _rows_type(flags))
+    _want(tokens, "tokens", torch.int32, (N,))
+    V, _ = _want_2d(dE, "dE", torch.float32 if flags & ALST_FLAG_DW_FP32 else torch.bfloat16)
+    _want_dw(dE, V, H, flags, "dE")
+    _want(workspace, "workspace", torch.uint8)
+    _call("alst_embedding_backward", dict(tokens=tokens, dy=dy, dE=dE, workspace=workspace),
+          _ptr(tokens), _ptr(dy), N, H, V, ignore_index, scale, _ptr(dE), _ptr(workspace), workspace.numel(), flags)
+
+
+def alst_block_norm_workspace_bytes(N: int, H: int) -> int:
+    return int(load_library().alst_block_norm_workspace_bytes(N, H))
+
+
+def alloc_block_norm_workspace(N: int, H: int, device="cuda") -> torch.Tensor:
+    nbytes = alst_block_norm_workspace_bytes(N, H)
+    if nbytes == 0:
+        raise AlstError(ALST_ERR_SHAPE, "alst_block_norm_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _want_gate(gate, N: int, H: int) -> int:
+    """gate_cols of a gate [N], [N,1] or [N,H]."""
+    if gate is None:
+        return 0
+    _want(gate, "gate", torch.bfloat16)
+    if tuple(gate.shape) in ((N,), (N, 1)):
+        return 1
+    _want(gate, "gate", torch.bfloat16, (N, H))
+    return H
+
+
+def alst_block_norm_forward(residual, *, branch=None, w_post=None, gate=None, w_pre=None, branch_scale: float = 1.0,
+                            eps: float = 1e-6, weight_offset: float = 0.0, residual_out=None, normed=None,
+                            flags: int = 0) -> None:
+    """residual_out = residual + branch_scale * sigmoid(gate) * norm(branch) * (w_post + weight_offset),
+    normed = norm(residual_out) * (w_pre + weight_offset); every part is optional (alst_block_norm.h)."""
+    rows, bf16 = _rows_type(flags), torch.bfloat16
+    N, H = _want_2d(residual, "residual", rows)
+    _want(branch, "branch", bf16, (N, H), optional=True)
+    _want(w_post, "w_post", bf16, (H,), optional=True)
+    _want(w_pre, "w_pre", bf16, (H,), optional=True)
+    _want(residual_out, "residual_out", rows, (N, H), optional=True)
+    _want(normed, "normed", bf16, (N, H), optional=True)
+    cols = _want_gate(gate, N, H)
+    _call("alst_block_norm_forward", dict(residual=residual, branch=branch, w_post=w_post, gate=gate, w_pre=w_pre,
+                                          residual_out=residual_out, normed=normed),
+          _ptr(residual), _ptr(branch), _ptr(w_post), _ptr(gate), cols, _ptr(w_pre), N, H, branch_scale, eps,
+          weight_offset, _ptr(residual_out), _ptr(normed), flags)
+
+
+def alst_block_norm_backward(residual_out, *, branch=None, w_post=None, gate=None, w_pre=None, d_normed=None,
+                             d_residual_out=None, branch_scale: float = 1.0, eps: float = 1e-6,
+                             weight_offset: float = 0.0, d_residual=None, d_branch=None, d_gate=None, dw_post=None,
+                             dw_pre=None, workspace=None, flags: int = 0) -> None:
+    """Gradients of alst_block_norm_forward from the residual_out that it wrote (alst_block_norm.h).  Without w_pre,
+    residual_out is not read and may be None."""
+    rows, bf16 = _rows_type(flags), torch.bfloat16
+    shaped = residual_out if residual_out is not None else d_residual_out
+    N, H = _want_2d(shaped, "residual_out" if residual_out is not None else "d_residual_out", rows)
+    for t, name, dtype in ((d_residual_out, "d_residual_out", rows), (d_residual, "d_residual", rows),
+                           (branch, "branch", bf16), (d_normed, "d_normed", bf16), (d_branch, "d_branch", bf16)):
+        _want(t, name, dtype, (N, H), optional=True)
+    _want(w_post, "w_post", bf16, (H,), optional=True)
+    _want(w_pre, "w_pre", bf16, (H,), optional=True)
+    cols = _want_gate(gate, N, H)
+    if gate is not None:
+        _want(d_gate, "d_gate", bf16, tuple(gate.shape))
+    sums = torch.float32 if flags & ALST_FLAG_DW_FP32 else bf16
+    _want(dw_post, "dw_post", sums, (H,), optional=True)
+    _want(dw_pre, "dw_pre", sums, (H,), optional=True)
+    _want(workspace, "workspace", torch.uint8, optional=True)
+    _call("alst_block_norm_backward",
+          dict(residual_out=residual_out, branch=branch, w_post=w_post, gate=gate, w_pre=w_pre, d_normed=d_normed,
+               d_residual_out=d_residual_out, d_residual=d_residual, d_branch=d_branch, d_gate=d_gate, dw_post=dw_post,
+               dw_pre=dw_pre, workspace=workspace),
+          _ptr(residual_out), _ptr(branch), _ptr(w_post), _ptr(gate), cols, _ptr(w_pre), _ptr(d_normed),
+          _ptr(d_residual_out), N, H, branch_scale, eps, weight_offset, _ptr(d_residual), _ptr(d_branch), _ptr(d_gate),
+          _ptr(dw_post), _ptr(dw_pre), _ptr(workspace), 0 if workspace is None else workspace.numel(), flags)
+
+
+class GradTensors:
+    """A list of gradients (bf16 and fp32, any shapes, dense) as alst_grad_norm and alst_grad_clip take it, checked and
+    marshalled once: a training program makes it after allocating its gradients.  outs: where the clipped gradients go
+    (None: in place).  Keeps the tensors alive."""
+
+    def __init__(self, grads, outs=None):
+        self.grads, self.outs = list(grads), list(grads if outs is None else outs)
+        if len(self.grads) != len(self.outs):
+            raise TypeError(f"{len(self.grads)} gradients and {len(self.outs)} outs")
+        self.array = (GradTensor * max(1, len(self.grads)))()
+        for k, (g, o) in enumerate(zip(self.grads, self.outs)):
+            if not isinstance(g, torch.Tensor) or g.dtype not in (torch.bfloat16, torch.float32):
+                raise TypeError(f"gradient {k}: must be a bfloat16 or float32 tensor")
+            _want(g, f"gradient {k}", g.dtype)
+            _want(o, f"out {k}", g.dtype, tuple(g.shape))
+            self.array[k] = GradTensor(g.data_ptr(), o.data_ptr(), g.numel(), int(g.dtype == torch.float32), 0)
+        for k, (g, o) in enumerate(zip(self.grads, self.outs)):
+            _on_device(**{f"gradient {k}": g, f"out {k}": o})
+        devices = {t.device for t in self.grads + self.outs}
+        if len(devices) > 1:
+            raise TypeError(f"gradients on different devices: {sorted(str(d) for d in devices)}")
+
+    def __len__(self):
+        return len(self.grads)
+
+
+def _want_grads(grads) -> GradTensors:
+    return grads if isinstance(grads, GradTensors) else GradTensors(grads)
+
+
+def alst_grad_norm_workspace_bytes(count: int) -> int:
+    return int(load_library().alst_grad_norm_workspace_bytes(count))
+
+
+def alloc_grad_norm_workspace(grads, device="cuda") -> torch.Tensor:
+    nbytes = alst_grad_norm_workspace_bytes(len(grads))
+    if nbytes == 0:
+        raise AlstError(ALST_ERR_SHAPE, "alst_grad_norm_workspace_bytes")
+    return torch.empty(nbytes, dtype=torch.uint8, device=device)
+
+
+def _grads_call(where: str, grads: GradTensors, tensors: dict, *args) -> None:
+    first = {"gradients": grads.grads[0]} if len(grads) else {}
+    _call(where, {**first, **tensors}, grads.array, len(grads), *args)
+
+
+def alst_grad_norm(grads, *, sumsq_out, norm_out=None, workspace) -> None:
+    """sumsq_out [1] f64 = the sum of the squares of all gradients (a GradTensors, or tensors), norm_out [1] f32 its root."""
+    grads = _want_grads(grads)
+    _want(sumsq_out, "sumsq_out", torch.float64, (1,))
+    _want(norm_out, "norm_out", torch.float32, (1,), optional=True)
+    _want(workspace, "workspace", torch.uint8)
+    _grads_call("alst_grad_norm", grads, dict(sumsq_out=sumsq_out, norm_out=norm_out, workspace=workspace),
+                _ptr(sumsq_out), _ptr(norm_out), _ptr(workspace), workspace.numel())
+
+
+def alst_grad_clip(grads, sumsq, max_norm: float, *, norm_out=None) -> None:
+    """Scales all gradients by min(1, max_norm / sqrt(sumsq)), in place or into the GradTensors' outs."""
+    grads = _want_grads(grads)
+    _want(sumsq, "sumsq", torch.float64, (1,))
+    _want(norm_out, "norm_out", torch.float32, (1,), optional=True)
+    _grads_call("alst_grad_clip", grads, dict(sumsq=sumsq, norm_out=norm_out), _ptr(sumsq), max_norm, _ptr(norm_out))
+
+
+def alst_grad_norm_clip(grads, max_norm: float, *, sumsq_out=None, norm_out=None, workspace) -> None:
+    """alst_grad_norm and alst_grad_clip in one call."""
+    grads = _want_grads(grads)
+    _want(sumsq_out, "sumsq_out", torch.float64, (1,), optional=True)
+    _want(norm_out, "norm_out", torch.float32, (1,), optional=True)
+    _want(workspace, "workspace", torch.uint8)
+    _grads_call("alst_grad_norm_clip", grads, dict(sumsq_out=sumsq_out, norm_out=norm_out, workspace=workspace),
+                max_norm, _ptr(sumsq_out), _ptr(norm_out), _ptr(workspace), workspace.numel())
 
 
 PROFILE_KINDS = ("logits_gemm", "dhidden_gemm", "dw_gemm", "tile_small_kernels",

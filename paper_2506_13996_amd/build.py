@@ -10,6 +10,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libalst.so")
 
+SOURCES = ("tiled_ce.hip", "tiled_mlp.hip", "embedding.hip", "block_norm.hip", "grads.hip", "prof.hip")
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
@@ -25,7 +26,7 @@ def hipcc_path() -> str:
 
 
 def build_library(verbose: bool = True) -> str:
-    srcs = [os.path.join(CSRC, f) for f in ("tiled_ce.hip", "tiled_mlp.hip", "prof.hip")]
+    srcs = [os.path.join(CSRC, f) for f in SOURCES]
     cmd = [hipcc_path(), *HIPCC_FLAGS, "-I", os.path.join(PKG_DIR, "..", "include"), *srcs,
            "-o", LIB_PATH + ".tmp"]
     if verbose:
