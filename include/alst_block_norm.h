@@ -39,7 +39,7 @@ extern "C" {
 #endif
 
 /* Bytes of device scratch that alst_block_norm_backward needs (partial sums of the weight gradients, at most
- * 8 H bytes for each of 1024 workgroups), 0 if the shape is invalid.  Pure host arithmetic. */
+ * 8 H bytes for each of 256 workgroups), 0 if the shape is invalid.  Pure host arithmetic. */
 size_t alst_block_norm_workspace_bytes(int64_t N, int64_t H);
 
 /*

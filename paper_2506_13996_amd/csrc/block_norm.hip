@@ -1,8 +1,11 @@
 // The norms around a block with its gate and scaled residual addition (alst_block_norm.h), forward and backward.
 //
 // A row is held in the registers of W wavefronts, 8 * VPT values a lane, so that everything is read and written once; its
-// sums (mean squares, and in backward the two products of a norm's gradient) go over the wavefronts through LDS.  A
-// workgroup holds R = max(1, 4 / W) rows at a time and walks the rows of the call.
+// sums (mean squares, and in backward the two products of a norm's gradient) go over the wavefronts through LDS.  Both are
+// bound by HBM: forward at 32768 x 4096 (norms before and after, 1.07 GB) 184 us = 5.8 TB/s, backward at 256000 x 4096 (12.6 GB)
+// 2.34 ms = 5.4 TB/s, of the 5.5 to 5.7 that a kernel reaches here that only reads four matrices and writes two.
+// Values stay packed bf16 in the registers between the passes over a row (stay_packed, made_here): with the conversions and
+// sums where the compiler puts them backward needs twice the registers and took 5.3 ms.
 #include <algorithm>
 
 #include "../../include/alst_block_norm.h"
@@ -11,7 +14,10 @@
 namespace alst {
 
 constexpr int64_t kMaxNormH = 16384;
-constexpr int kMaxNormParts = 1024;            // workgroups of a backward launch: rows of partial weight gradients
+// Workgroups of a backward launch, each with its rows of partial weight gradients: one a compute unit.  More of them keep more
+// rows open at once than memory likes: 256000 x 4096 2.34 ms, 2.54 with 512 and 2.82 with 1024 workgroups of four wavefronts.
+constexpr int kMaxNormParts = 256;
+constexpr int kPlaces = 2 * 16;                // of a row's sums: two turns of up to 16 wavefronts
 
 struct NormParams {
     const void *residual, *d_residual_out;
@@ -27,236 +33,277 @@ struct NormParams {
 // A workgroup's place: R rows of W wavefronts.
 struct RowPlace {
     int W, R, row, tid;                        // tid: thread of the row
-    float* lds;                                // [2][R][W][2]
+    float4* lds;                               // [2][R][16]
     int turn;
-    __device__ __forceinline__ RowPlace(float* lds_) : W(blockDim.x >> 6), R(blockDim.y), row(threadIdx.y), tid(threadIdx.x), lds(lds_), turn(0) {}
-    // Sums of two values over the row.  The room alternates, so a sum's readers are done when its room comes up again.
-    __device__ __forceinline__ void sum2(float& a, float& b) {
-        a = wave_sum(a);
-        b = wave_sum(b);
+    __device__ __forceinline__ RowPlace(float* lds_)
+        : W(blockDim.x >> 6), R(blockDim.y), row(__builtin_amdgcn_readfirstlane(threadIdx.y)), tid(threadIdx.x),
+          lds(reinterpret_cast<float4*>(lds_)), turn(0) {}
+    // Sums of K values over the row: over a wavefront's lanes, then over the row's wavefronts.  The room alternates, so a
+    // sum's readers are done when its room comes up again.
+    template <int K>
+    __device__ __forceinline__ void sum(float (&v)[K]) {
+        static_assert(K <= 4, "a place holds four values");
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = wave_sum(v[k]);
         if (W == 1) return;
-        float* const at = lds + (turn * R + row) * W * 2;
+        float4* const at = lds + (turn * R + row) * 16;
         turn ^= 1;
-        if ((tid & 63) == 0) {
-            at[(tid >> 6) * 2] = a;
-            at[(tid >> 6) * 2 + 1] = b;
-        }
+        const int lane = tid & 63;
+        if (lane == 0) at[tid >> 6] = make_float4(v[0], K > 1 ? v[1] : 0.f, K > 2 ? v[2] : 0.f, K > 3 ? v[3] : 0.f);
         __syncthreads();
-        a = b = 0.f;
-        for (int w = 0; w < W; ++w) {
-            a += at[w * 2];
-            b += at[w * 2 + 1];
-        }
-    }
-    __device__ __forceinline__ void sum1(float& a) {
-        float none = 0.f;
-        sum2(a, none);
+        const float4 q = (lane & 15) < W ? at[lane & 15] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int k = 0; k < K; ++k) v[k] = sum_of_16((&q.x)[k]);
     }
 };
 
-// sigmoid(z) and 1 - sigmoid(z), both to a few steps of fp32 however large |z| is.
+// sigmoid(z) and 1 - sigmoid(z), both to a few steps of fp32 however large |z| is: from t = exp(-|z|), whose exponent is
+// formed in two parts (v_exp_f32 is exact to a step, the product with log2 e is not), and 1 / (1 + t) by one step of Newton's
+// iteration, which gives the bits of the quotient or their neighbours at a third of its instructions.  32768 x 5120
+// backward with a gate for each element, otherwise as it was then: 1302 us with expf and the quotient, 1173 like this.
 struct Gate { float on, off; };
 __device__ __forceinline__ Gate gate_of(float z) {
-    const float t = expf(-fabsf(z)), s = 1.f / (1.f + t);
-    return z >= 0.f ? Gate{s, t * s} : Gate{t * s, s};
+    constexpr float kLog2e = 1.44269502e+00f, kLog2eRest = 1.92596299e-08f, kLn2 = 6.93147182e-01f;
+    float a = -fabsf(z);
+    a = a < -150.f ? -150.f : a;              // (exp is 0 in fp32 from there on, and NaN stays)
+    const float hi = a * kLog2e, lo = fmaf(a, kLog2eRest, fmaf(a, kLog2e, -hi));
+    const float e = __builtin_amdgcn_exp2f(hi), t = fmaf(e, lo * kLn2, e);
+    const float d = 1.f + t;
+    float s = __builtin_amdgcn_rcpf(d);
+    s = fmaf(fmaf(-d, s, 1.f), s, s);
+    return z < 0.f ? Gate{t * s, s} : Gate{s, t * s};
 }
 __device__ __forceinline__ float bf16_value(const uint16_t* p) { return __uint_as_float((uint32_t)*p << 16); }
 
-template <bool F32, int VPT>
-__global__ __launch_bounds__(1024) void norm_forward_kernel(NormParams p) {
+// Columns of a lane, and a weight's values there (without the weight: ones, whatever the offset).
+template <int VPT>
+struct Columns {
+    uint32_t at[VPT];
+    __device__ __forceinline__ Columns(const RowPlace& place) {
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) at[v] = (v * (place.W * 64) + place.tid) * 8;
+    }
+    __device__ __forceinline__ void weight(Raw8<false> (&w)[VPT], const uint16_t* p, int H) const {
+        const RowBuffer<false> row(p, 0, H, true);
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) w[v] = p ? row.load(at[v]) : Raw8<false>{make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u)};
+    }
+};
+
+// DENSE: a gate for each element.  Absent matrices read as zeros, absent weights as ones: the arithmetic has no branches.
+template <bool F32, bool DENSE, int VPT>
+__global__ __launch_bounds__(VPT == 1 ? 1024 : 512) void norm_forward_kernel(NormParams p) {
     extern __shared__ float lds[];
     RowPlace at(lds);
+    const Columns<VPT> col(at);
     const float inv_h = 1.f / p.H;
-    int col[VPT];
-    bool in[VPT];
+    const bool pre = p.w_pre != nullptr, post = p.w_post != nullptr, row_gated = !DENSE && p.gate_cols == 1;
+    const float o1 = post ? p.offset : 0.f;
     Raw8<false> w1[VPT], w2[VPT];
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-        col[v] = (v * (at.W * 64) + at.tid) * 8;
-        in[v] = col[v] < p.H;
-        w1[v] = p.w_post && in[v] ? load8<false>(p.w_post, col[v]) : zero8<false>();
-        w2[v] = p.w_pre && in[v] ? load8<false>(p.w_pre, col[v]) : zero8<false>();
-    }
+    col.weight(w1, p.w_post, p.H);
+    col.weight(w2, p.w_pre, p.H);
     for (int64_t i0 = (int64_t)blockIdx.x * at.R; i0 < p.N; i0 += (int64_t)gridDim.x * at.R) {
-        const int64_t i = i0 + at.row, base = i * p.H;
+        const int64_t i = i0 + at.row;
         const bool row_in = i < p.N;
+        const RowBuffer<F32> residual(p.residual, i, p.H, row_in), residual_out(p.residual_out, i, p.H, row_in);
+        const RowBuffer<false> branch(p.branch, i, p.H, row_in), gate(DENSE ? p.gate : nullptr, i, p.H, row_in),
+            normed(p.normed, i, p.H, row_in);
         Raw8<F32> r[VPT];
         Raw8<false> b[VPT], z[VPT];
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
-            const bool here = row_in && in[v];
-            r[v] = here ? load8<F32>(p.residual, base + col[v]) : zero8<F32>();
-            b[v] = here && p.branch ? load8<false>(p.branch, base + col[v]) : zero8<false>();
-            z[v] = here && p.gate_cols > 1 ? load8<false>(p.gate, base + col[v]) : zero8<false>();
+            r[v] = residual.load(col.at[v]);
+            b[v] = branch.load(col.at[v]);
+            if (DENSE) z[v] = gate.load(col.at[v]);
+            stay_packed(w1[v]);
+            stay_packed(w2[v]);
         }
-        float x[VPT][8];
-        if (p.branch) {
-            float q1 = 1.f;
-            if (p.w_post) {
-                float bb = 0.f;
-#pragma unroll
-                for (int v = 0; v < VPT; ++v)
-#pragma unroll
-                    for (int k = 0; k < 8; ++k) bb += b[v].get(k) * b[v].get(k);
-                at.sum1(bb);
-                q1 = 1.f / sqrtf(bb * inv_h + p.eps);
-            }
-            const float s = p.gate_cols == 1 && row_in ? p.scale * gate_of(bf16_value(p.gate + i)).on : p.scale;
-#pragma unroll
-            for (int v = 0; v < VPT; ++v) {
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    float change = s * b[v].get(k);
-                    if (p.w_post) change *= q1 * (w1[v].get(k) + p.offset);
-                    if (p.gate_cols > 1) change *= gate_of(z[v].get(k)).on;
-                    x[v][k] = r[v].get(k) + change;
-                }
-                if (row_in && in[v]) store8<F32>(p.residual_out, base + col[v], x[v]);
-            }
-        } else {
+        float s = p.scale;
+        if (row_gated && row_in) s *= gate_of(bf16_value(p.gate + i)).on;
+        if (post) {
+            float bb[1] = {};
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) x[v][k] = r[v].get(k);
+                for (int k = 0; k < 8; ++k) bb[0] = fmaf(b[v].get(k), b[v].get(k), bb[0]);
+            at.sum(bb);
+            s *= 1.f / sqrtf(bb[0] * inv_h + p.eps);
         }
-        if (p.w_pre) {
-            float xx = 0.f;
+        float x[VPT][8], xx[1] = {};
 #pragma unroll
-            for (int v = 0; v < VPT; ++v)
+        for (int v = 0; v < VPT; ++v) {
+            stay_packed(b[v]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k) xx += x[v][k] * x[v][k];
-            at.sum1(xx);
-            const float q2 = 1.f / sqrtf(xx * inv_h + p.eps);
+            for (int k = 0; k < 8; ++k) {
+                float change = s * b[v].get(k) * (w1[v].get(k) + o1);
+                if (DENSE) change *= gate_of(z[v].get(k)).on;
+                x[v][k] = r[v].get(k) + change;
+                xx[0] = fmaf(x[v][k], x[v][k], xx[0]);
+            }
+            residual_out.store(col.at[v], x[v]);
+        }
+        if (pre) {
+            at.sum(xx);
+            const float q2 = 1.f / sqrtf(xx[0] * inv_h + p.eps);
 #pragma unroll
             for (int v = 0; v < VPT; ++v) {
                 float n[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) n[k] = x[v][k] * q2 * (w2[v].get(k) + p.offset);
-                if (row_in && in[v]) store8<false>(p.normed, base + col[v], n);
+                normed.store(col.at[v], n);
             }
         }
     }
 }
 
-template <bool F32, int VPT>
-__global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
+template <bool F32, bool DENSE, int VPT>
+__global__ __launch_bounds__(VPT == 1 ? 1024 : 512) void norm_backward_kernel(NormParams p) {
     extern __shared__ float lds[];
     RowPlace at(lds);
+    const Columns<VPT> col(at);
     const float inv_h = 1.f / p.H;
-    int col[VPT];
-    bool in[VPT];
+    const bool pre = p.w_pre != nullptr, post = p.w_post != nullptr, row_gated = !DENSE && p.gate_cols == 1;
+    const float o1 = post ? p.offset : 0.f;
     Raw8<false> w1[VPT], w2[VPT];
-    float dw1[VPT][8], dw2[VPT][8];
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-        col[v] = (v * (at.W * 64) + at.tid) * 8;
-        in[v] = col[v] < p.H;
-        w1[v] = p.w_post && in[v] ? load8<false>(p.w_post, col[v]) : zero8<false>();
-        w2[v] = p.w_pre && in[v] ? load8<false>(p.w_pre, col[v]) : zero8<false>();
-#pragma unroll
-        for (int k = 0; k < 8; ++k) dw1[v][k] = dw2[v][k] = 0.f;
-    }
-    const bool post = p.w_post != nullptr, gated = p.gate_cols != 0;
-    for (int64_t i0 = (int64_t)blockIdx.x * at.R; i0 < p.N; i0 += (int64_t)gridDim.x * at.R) {
-        const int64_t i = i0 + at.row, base = i * p.H;
-        const bool row_in = i < p.N;
+    col.weight(w1, p.w_post, p.H);
+    col.weight(w2, p.w_pre, p.H);
+    float dw1[VPT][8] = {}, dw2[VPT][8] = {};
+    // The next row is asked for before this one is worked on, into other registers: one workgroup a compute unit keeps the
+    // memory busy, and few rows are open at a time.  (Four groups a lane leave no registers for that.)
+    constexpr bool AHEAD = VPT == 1;
+    struct Row {
         Raw8<F32> r[VPT], up[VPT];
-        Raw8<false> b[VPT], dn[VPT], z[VPT];
+        Raw8<false> dn[VPT], b[VPT], z[VPT];
+        uint16_t gate;
+    };
+    auto load = [&](Row& row, int64_t i) {
+        const bool row_in = i < p.N;
+        const RowBuffer<F32> r(p.residual, i, p.H, row_in), up(p.d_residual_out, i, p.H, row_in);
+        const RowBuffer<false> dn(p.d_normed, i, p.H, row_in), b(p.branch, i, p.H, row_in), z(DENSE ? p.gate : nullptr, i, p.H, row_in);
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
-            const bool here = row_in && in[v];
-            r[v] = here && p.w_pre ? load8<F32>(p.residual, base + col[v]) : zero8<F32>();
-            dn[v] = here && p.w_pre ? load8<false>(p.d_normed, base + col[v]) : zero8<false>();
-            up[v] = here && p.d_residual_out ? load8<F32>(p.d_residual_out, base + col[v]) : zero8<F32>();
-            b[v] = here && (post || gated) ? load8<false>(p.branch, base + col[v]) : zero8<false>();
-            z[v] = here && p.gate_cols > 1 ? load8<false>(p.gate, base + col[v]) : zero8<false>();
+            row.r[v] = r.load(col.at[v]);
+            row.dn[v] = dn.load(col.at[v]);
+            row.b[v] = b.load(col.at[v]);
+            row.up[v] = up.load(col.at[v]);
+            if (DENSE) row.z[v] = z.load(col.at[v]);
         }
-        float bb = 0.f, q1 = 1.f;
-        if (post) {
+        row.gate = row_gated && row_in ? p.gate[i] : 0;
+    };
+    auto work = [&](Row& row, int64_t i) {
+        const bool row_in = i < p.N;
+        auto &r = row.r, &up = row.up;
+        auto &dn = row.dn, &b = row.b, &z = row.z;
+        const RowBuffer<F32> d_residual(p.d_residual, i, p.H, row_in);
+        const RowBuffer<false> d_branch(p.d_branch, i, p.H, row_in), d_gate(DENSE ? p.d_gate : nullptr, i, p.H, row_in);
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            stay_packed(w1[v]);
+            stay_packed(w2[v]);
+        }
+        // the sums that need no other: of r'^2, of dn (w_pre + o) r', of b^2
+        float s1[3] = {};
+        if (pre || post) {
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
 #pragma unroll
-                for (int k = 0; k < 8; ++k) bb += b[v].get(k) * b[v].get(k);
-            at.sum1(bb);
-            q1 = 1.f / sqrtf(bb * inv_h + p.eps);
+                for (int k = 0; k < 8; ++k) {
+                    const float x = r[v].get(k), y = b[v].get(k);
+                    s1[0] = fmaf(x, x, s1[0]);
+                    s1[1] = fmaf(dn[v].get(k) * (w2[v].get(k) + p.offset), x, s1[1]);
+                    s1[2] = fmaf(y, y, s1[2]);
+                }
+            at.sum(s1);
         }
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            stay_packed(r[v]);
+            stay_packed(dn[v]);
+            stay_packed(b[v]);
+            stay_packed(w2[v]);
+        }
+        const float q2 = 1.f / sqrtf(s1[0] * inv_h + p.eps), c2 = q2 * q2 * s1[1] * inv_h;
+        const float q1 = post ? 1.f / sqrtf(s1[2] * inv_h + p.eps) : 1.f;
         float g[VPT][8];                       // dr
-        if (p.w_pre) {
-            float rr = 0.f, ur = 0.f;
 #pragma unroll
-            for (int v = 0; v < VPT; ++v)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    rr += r[v].get(k) * r[v].get(k);
-                    ur += dn[v].get(k) * (w2[v].get(k) + p.offset) * r[v].get(k);
-                }
-            at.sum2(rr, ur);
-            const float q2 = 1.f / sqrtf(rr * inv_h + p.eps), c = q2 * q2 * ur * inv_h;
-#pragma unroll
-            for (int v = 0; v < VPT; ++v)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) {
-                    g[v][k] = up[v].get(k) + q2 * (dn[v].get(k) * (w2[v].get(k) + p.offset) - r[v].get(k) * c);
-                    dw2[v][k] += dn[v].get(k) * (r[v].get(k) * q2);
-                }
-        } else {
-#pragma unroll
-            for (int v = 0; v < VPT; ++v)
-#pragma unroll
-                for (int k = 0; k < 8; ++k) g[v][k] = up[v].get(k);
-        }
-        if (p.d_residual) {
-#pragma unroll
-            for (int v = 0; v < VPT; ++v)
-                if (row_in && in[v]) store8<F32>(p.d_residual, base + col[v], g[v]);
-        }
-        if (!p.d_branch) continue;
-        // dp, in g's place; sum over the row of (dp without a row's gate factor) * (w_post + o) * b: of use to both the norm's and
-        // the row gate's gradient
-        const Gate row_gate = p.gate_cols == 1 && row_in ? gate_of(bf16_value(p.gate + i)) : Gate{1.f, 0.f};
-        const float s = p.scale * row_gate.on;
-        float vb = 0.f;
-        float off[VPT][8];
-#pragma unroll
-        for (int v = 0; v < VPT; ++v)
+        for (int v = 0; v < VPT; ++v) {
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const Gate gate = p.gate_cols > 1 ? gate_of(z[v].get(k)) : Gate{1.f, 0.f};
-                off[v][k] = gate.off;
-                g[v][k] *= s * gate.on;
-                if (post) dw1[v][k] += g[v][k] * (b[v].get(k) * q1);
-                vb += g[v][k] * (post ? w1[v].get(k) + p.offset : 1.f) * b[v].get(k);
+                const float x = r[v].get(k), d = dn[v].get(k);
+                g[v][k] = fmaf(q2, fmaf(d, w2[v].get(k) + p.offset, -x * c2), up[v].get(k));
+                dw2[v][k] = fmaf(d, x * q2, dw2[v][k]);
             }
-        if (post || p.gate_cols == 1) at.sum1(vb);
-        if (p.gate_cols == 1 && row_in && at.tid == 0) {
-            const __bf16 dz = (__bf16)(row_gate.off * q1 * vb);
+            made_here(dw2[v]);
+            d_residual.store(col.at[v], g[v]);
+        }
+        // dp, in g's place, and the sum over the row of dp (w_post + o) b: the norm's gradient and a row's gate both take it
+        const Gate row_gate = row_gated ? gate_of(__uint_as_float((uint32_t)row.gate << 16)) : Gate{1.f, 0.f};
+        const float s = p.scale * row_gate.on;
+        float vb[1] = {};
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const float y = b[v].get(k);
+                g[v][k] *= DENSE ? s * gate_of(z[v].get(k)).on : s;
+                dw1[v][k] = fmaf(g[v][k], y * q1, dw1[v][k]);
+                vb[0] = fmaf(g[v][k] * (w1[v].get(k) + o1), y, vb[0]);
+            }
+            made_here(dw1[v]);
+        }
+        if (post || row_gated) at.sum(vb);
+#pragma unroll
+        for (int v = 0; v < VPT; ++v) {
+            stay_packed(b[v]);
+            stay_packed(w1[v]);
+            if (DENSE && VPT > 1) stay_packed(z[v]);
+        }
+        if (row_gated && row_in && at.tid == 0) {
+            const __bf16 dz = (__bf16)(row_gate.off * q1 * vb[0]);
             p.d_gate[i] = __builtin_bit_cast(uint16_t, dz);
         }
-        const float c = q1 * q1 * vb * inv_h;
+        const float c1 = post ? q1 * q1 * vb[0] * inv_h : 0.f;
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
             float o[8], dz[8];
 #pragma unroll
             for (int k = 0; k < 8; ++k) {
-                const float w = post ? w1[v].get(k) + p.offset : 1.f;
-                if (p.gate_cols > 1) dz[k] = g[v][k] * off[v][k] * (q1 * w * b[v].get(k));
-                o[k] = post ? q1 * (g[v][k] * w - b[v].get(k) * c) : g[v][k];
+                const float w = w1[v].get(k) + o1, y = b[v].get(k);
+                if (DENSE) dz[k] = g[v][k] * gate_of(z[v].get(k)).off * (q1 * w * y);
+                o[k] = q1 * fmaf(g[v][k], w, -y * c1);
             }
-            if (row_in && in[v]) {
-                store8<false>(p.d_branch, base + col[v], o);
-                if (p.gate_cols > 1) store8<false>(p.d_gate, base + col[v], dz);
-            }
+            d_branch.store(col.at[v], o);
+            if (DENSE) d_gate.store(col.at[v], dz);
+        }
+    };
+    const int64_t step = (int64_t)gridDim.x * at.R, first = (int64_t)blockIdx.x * at.R;
+    if constexpr (AHEAD) {
+        Row even, odd;
+        load(even, first + at.row);
+        for (int64_t i0 = first; i0 < p.N; i0 += 2 * step) {
+            const int64_t i = i0 + at.row;
+            load(odd, i + step);
+            work(even, i);
+            if (i0 + step >= p.N) break;
+            load(even, i + 2 * step);
+            work(odd, i + step);
+        }
+    } else {
+        for (int64_t i0 = first; i0 < p.N; i0 += step) {
+            Row row;
+            load(row, i0 + at.row);
+            work(row, i0 + at.row);
         }
     }
     // the rows of the workgroup together, then its partial sums of the weights' gradients
     float* const part = p.parts + (int64_t)blockIdx.x * 2 * p.H;
     for (int which = 0; which < 2; ++which) {
-        if (!(which ? post : p.w_pre != nullptr)) continue;
+        if (!(which ? post : pre)) continue;
         if (at.R > 1) {
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
-                if (in[v]) store8<true>(lds, (int64_t)at.row * p.H + col[v], which ? dw1[v] : dw2[v]);
+                if (col.at[v] < (uint32_t)p.H) store8<true>(lds + at.row * p.H, col.at[v], which ? dw1[v] : dw2[v]);
             __syncthreads();
             for (int c = at.row * blockDim.x + at.tid; c < p.H; c += blockDim.x * at.R) {
                 float t = 0.f;
@@ -266,32 +313,44 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
         } else {
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
-                if (in[v]) store8<true>(part, (int64_t)which * p.H + col[v], which ? dw1[v] : dw2[v]);
+                if (col.at[v] < (uint32_t)p.H) store8<true>(part + which * p.H, col.at[v], which ? dw1[v] : dw2[v]);
         }
     }
 }
 
-// Weight gradients: the workgroups' partial sums of 64 columns, 16 threads a column.
+// Weight gradients: the workgroups' partial sums of 64 columns.  16 lanes take the columns of a row, so that the workgroup
+// reads 64 rows at a time and a thread has its rows in flight together.
 __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restrict__ parts, int n, int H, void* dw_pre, void* dw_post,
                                                             bool f32, bool accumulate) {
-    __shared__ float lds[16][64];
-    const int lane = threadIdx.x & 63, y = threadIdx.x >> 6, which = blockIdx.y, c = blockIdx.x * 64 + lane;
+    __shared__ float lds[64][64 + 4];
+    const int which = blockIdx.y, x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4, c0 = blockIdx.x * 64;
     void* const out = which ? dw_post : dw_pre;
     if (!out) return;
-    float s = 0.f;
-    if (c < H)
-        for (int k = y; k < n; k += 16) s += parts[((int64_t)k * 2 + which) * H + c];
-    lds[y][lane] = s;
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+    if (c0 + x < H) {
+#pragma unroll 8
+        for (int k = y; k < n; k += 64) {
+            const float4 q = *reinterpret_cast<const float4*>(parts + ((int64_t)k * 2 + which) * H + c0 + x);
+            s.x += q.x; s.y += q.y; s.z += q.z; s.w += q.w;
+        }
+    }
+    *reinterpret_cast<float4*>(&lds[y][x]) = s;
     __syncthreads();
-    if (y == 0 && c < H) {
-        s = 0.f;
-        for (int k = 0; k < 16; ++k) s += lds[k][lane];
+    // 16 threads a column, four rows each, added up over lanes 64 apart
+    const int c = threadIdx.x & 63, part = threadIdx.x >> 6;
+    float t = lds[part * 4][c] + lds[part * 4 + 1][c] + (lds[part * 4 + 2][c] + lds[part * 4 + 3][c]);
+    __syncthreads();
+    lds[part][c] = t;
+    __syncthreads();
+    if (part == 0 && c0 + c < H) {
+        t = 0.f;
+        for (int k = 0; k < 16; ++k) t += lds[k][c];
         if (f32) {
-            float* const o = static_cast<float*>(out) + c;
-            *o = accumulate ? *o + s : s;
+            float* const o = static_cast<float*>(out) + c0 + c;
+            *o = accumulate ? *o + t : t;
         } else {
-            uint16_t* const o = static_cast<uint16_t*>(out) + c;
-            const __bf16 r = (__bf16)(accumulate ? bf16_value(o) + s : s);
+            uint16_t* const o = static_cast<uint16_t*>(out) + c0 + c;
+            const __bf16 r = (__bf16)(accumulate ? bf16_value(o) + t : t);
             *o = __builtin_bit_cast(uint16_t, r);
         }
     }
@@ -299,14 +358,27 @@ __global__ __launch_bounds__(1024) void norm_weights_kernel(const float* __restr
 
 // ---- host ----
 
+// Wavefronts of a row, rows of a workgroup, groups of eight values a lane.
 struct NormShape { int W, R, vpt; };
-static NormShape norm_shape(int64_t H) {
-    const int vpt = H <= 512 ? 1 : 2;
+static NormShape shape_of(int64_t H, int vpt, int waves) {
     const int W = (int)((H + 512 * vpt - 1) / (512 * vpt));
-    return {W, W == 1 ? 4 : W == 2 ? 2 : 1, vpt};
+    return {W, std::max(1, waves / W), vpt};
+}
+// Forward: two groups a lane (5120 columns in 5 wavefronts: 32768 rows 227 us, with one group in 10 wavefronts 266; 4096 columns
+// 184 and 182), one for rows of one wavefront, four above 8192 columns.
+static NormShape forward_shape(int64_t H) { return shape_of(H, H <= 512 ? 1 : H <= 8192 ? 2 : 4, 4); }
+// A workgroup for each row, so that the open rows are neighbours (32768 x 4096: 184 us, 209 with 2048 workgroups that walk); of short
+// rows a workgroup takes several, which pays for reading the weights (262144 x 256: 98 us, 136).
+static int64_t forward_grid(int64_t N, int64_t H, int R) { return std::min<int64_t>((N + R - 1) / R, H <= 512 ? 8192 : 1 << 22); }
+// Backward: a group a lane, so that the wavefronts of a row spread over the four SIMDs (5120 columns: 10 wavefronts; with two
+// groups 5, of which one SIMD has two: 32768 x 5120 with a gate for each element 620 us against 493) and 1024 threads have
+// the registers for two rows.  Above 8192 columns four groups, and a row at a time.  Rows of one wavefront, which wait for no other, come by 16
+// (262144 x 256: 184 us, 215 by 8).
+static NormShape backward_shape(int64_t H) {
+    return H <= 512 ? shape_of(H, 1, 16) : shape_of(H, H <= 8192 ? 1 : 4, 8);
 }
 static int64_t norm_parts(int64_t N, int64_t H) {
-    const NormShape s = norm_shape(H);
+    const NormShape s = backward_shape(H);
     return std::min<int64_t>((N + s.R - 1) / s.R, kMaxNormParts);
 }
 
@@ -348,12 +420,17 @@ int alst_block_norm_forward(const void* residual, const void* branch, const void
     const int rc = validate_norm(p, H, gate_cols);
     if (rc != ALST_OK) return rc;
     p.H = (int)H; p.gate_cols = (int)gate_cols;
-    const NormShape s = norm_shape(H);
+    const NormShape s = forward_shape(H);
     const bool f32 = flags & ALST_FLAG_RESIDUAL_FP32;
-    auto kernel = s.vpt == 1 ? (f32 ? norm_forward_kernel<true, 1> : norm_forward_kernel<false, 1>)
-                             : (f32 ? norm_forward_kernel<true, 2> : norm_forward_kernel<false, 2>);
-    const int64_t grid = std::min<int64_t>((N + s.R - 1) / s.R, 256 * 8);
-    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(s.W * 64, s.R), 2 * s.R * s.W * 2 * sizeof(float), (hipStream_t)stream, p);
+    using Kernel = void (*)(NormParams);
+    static const Kernel kernels[2][2][3] = {
+        {{norm_forward_kernel<false, false, 1>, norm_forward_kernel<false, false, 2>, norm_forward_kernel<false, false, 4>},
+         {norm_forward_kernel<false, true, 1>, norm_forward_kernel<false, true, 2>, norm_forward_kernel<false, true, 4>}},
+        {{norm_forward_kernel<true, false, 1>, norm_forward_kernel<true, false, 2>, norm_forward_kernel<true, false, 4>},
+         {norm_forward_kernel<true, true, 1>, norm_forward_kernel<true, true, 2>, norm_forward_kernel<true, true, 4>}}};
+    const Kernel kernel = kernels[f32][gate_cols > 1][s.vpt >> 1];
+    const int64_t grid = forward_grid(N, H, s.R);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(s.W * 64, s.R), kPlaces * s.R * sizeof(float4), (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? ALST_OK : ALST_ERR_HIP;
 }
 
@@ -378,12 +455,16 @@ int alst_block_norm_backward(const void* residual_out, const void* branch, const
     if (rc == ALST_OK && (w_pre || w_post) && workspace_bytes < alst_block_norm_workspace_bytes(N, H)) rc = ALST_ERR_WORKSPACE;
     if (rc != ALST_OK) return rc;
     p.H = (int)H; p.gate_cols = (int)gate_cols;
-    const NormShape s = norm_shape(H);
+    const NormShape s = backward_shape(H);
     const bool f32 = flags & ALST_FLAG_RESIDUAL_FP32;
-    auto kernel = s.vpt == 1 ? (f32 ? norm_backward_kernel<true, 1> : norm_backward_kernel<false, 1>)
-                             : (f32 ? norm_backward_kernel<true, 2> : norm_backward_kernel<false, 2>);
+    using Kernel = void (*)(NormParams);
+    static const Kernel kernels[2][2][2] = {{{norm_backward_kernel<false, false, 1>, norm_backward_kernel<false, false, 4>},
+                                             {norm_backward_kernel<false, true, 1>, norm_backward_kernel<false, true, 4>}},
+                                            {{norm_backward_kernel<true, false, 1>, norm_backward_kernel<true, false, 4>},
+                                             {norm_backward_kernel<true, true, 1>, norm_backward_kernel<true, true, 4>}}};
+    const Kernel kernel = kernels[f32][gate_cols > 1][s.vpt > 1];
     const int grid = (int)norm_parts(N, H);
-    const size_t lds = std::max<size_t>(2 * s.R * s.W * 2, s.R > 1 ? s.R * H : 0) * sizeof(float);
+    const size_t lds = std::max<size_t>(kPlaces * s.R * sizeof(float4), s.R > 1 ? s.R * H * sizeof(float) : 0);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(s.W * 64, s.R), lds, (hipStream_t)stream, p);
     if (w_pre || w_post)
         hipLaunchKernelGGL(norm_weights_kernel, dim3((unsigned)((H + 63) / 64), 2), dim3(1024), 0, (hipStream_t)stream, (const float*)p.parts,

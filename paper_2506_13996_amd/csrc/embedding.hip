@@ -25,11 +25,11 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(const int32_t* _
         const bool named = t >= 0 && t < V, kept = named && t != ignore_index;
         if (!named && t != ignore_index && status && (threadIdx.x & 63) == 0 && blockIdx.y == 0) *status = ALST_ERR_LABEL_RANGE;
         if (col >= H) continue;
-        const Raw8<false> r = kept ? load8<false>(E, (int64_t)t * H + col) : zero8<false>();
+        const Raw8<false> r = kept ? load8<false>(row_of<false>(E, (int64_t)t * H), col) : zero8<false>();
         float v[8];
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = kept ? r.get(k) * scale : 0.f;
-        store8<F32>(y, i * H + col, v);
+        store8<F32>(row_of<F32>(y, i * H), col, v);
     }
 }
 
@@ -155,20 +155,20 @@ __device__ __forceinline__ void write_grad(const Grad& g, int64_t at, const floa
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = sum[k] * g.scale;
         if (g.accumulate) {
-            const Raw8<true> old = load8<true>(g.dE, at);
+            const Raw8<true> old = load8<true>(row_of<true>(g.dE, at), 0);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] += old.get(k);
         }
-        store8<true>(g.dE, at, v);
+        store8<true>(row_of<true>(g.dE, at), 0, v);
     } else {
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] = sum[k] * g.scale;
         if (g.accumulate) {
-            const Raw8<false> old = load8<false>(g.dE, at);
+            const Raw8<false> old = load8<false>(row_of<false>(g.dE, at), 0);
 #pragma unroll
             for (int k = 0; k < 8; ++k) v[k] += old.get(k);
         }
-        store8<false>(g.dE, at, v);
+        store8<false>(row_of<false>(g.dE, at), 0, v);
     }
 }
 
@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const Pair* __restrict__ 
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const int key = __builtin_amdgcn_readlane(mine.key, j0 + j), row = __builtin_amdgcn_readlane(mine.row, j0 + j);
-            r[j] = key < V && col < H ? load8<F32>(dy, (int64_t)row * H + col) : zero8<F32>();
+            r[j] = key < V && col < H ? load8<F32>(row_of<F32>(dy, (int64_t)row * H), col) : zero8<F32>();
         }
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -208,8 +208,8 @@ __global__ __launch_bounds__(256) void run_sums_kernel(const Pair* __restrict__ 
             const bool last = at + 1 == rows;
             if (key == behind && !last) continue;
             if (col < H) {
-                if (came) store8<true>(parts, (range * 2) * H + col, sum);
-                else if (key == behind) store8<true>(parts, (range * 2 + 1) * H + col, sum);
+                if (came) store8<true>(parts + range * 2 * H, col, sum);
+                else if (key == behind) store8<true>(parts + (range * 2 + 1) * H, col, sum);
                 else write_grad(g, (int64_t)key * H + col, sum);
             }
             if (last) return;
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(64) void join_kernel(const Pair* __restrict__ pairs
     float sum[8] = {};
     auto add = [&](int64_t slot) {
         if (col >= H) return;
-        const Raw8<true> r = load8<true>(parts, slot * H + col);
+        const Raw8<true> r = load8<true>(parts + slot * H, col);
 #pragma unroll
         for (int k = 0; k < 8; ++k) sum[k] += r.get(k);
     };

@@ -23,15 +23,22 @@ template <> struct Raw8<true> {
     __device__ __forceinline__ float get(int i) const { return (&q[i >> 2].x)[i & 3]; }
 };
 
+// A row of a matrix: a base that is the same for a wavefront, so that its elements are addressed by a scalar base and a 32-bit
+// offset of the lane.
+template <bool F32> __device__ __forceinline__ const char* row_of(const void* p, int64_t at) {
+    return static_cast<const char*>(p) + at * (F32 ? 4 : 2);
+}
+template <bool F32> __device__ __forceinline__ char* row_of(void* p, int64_t at) { return static_cast<char*>(p) + at * (F32 ? 4 : 2); }
+
 template <bool F32>
-__device__ __forceinline__ Raw8<F32> load8(const void* p, int64_t at) {      // element `at`, a multiple of 8
+__device__ __forceinline__ Raw8<F32> load8(const void* row, uint32_t at) {      // element `at` of the row, a multiple of 8
     Raw8<F32> r;
+    const char* const from = static_cast<const char*>(row) + (size_t)(at * (F32 ? 4u : 2u));
     if constexpr (F32) {
-        const float4* f = reinterpret_cast<const float4*>(reinterpret_cast<const float*>(p) + at);
-        r.q[0] = f[0];
-        r.q[1] = f[1];
+        r.q[0] = reinterpret_cast<const float4*>(from)[0];
+        r.q[1] = reinterpret_cast<const float4*>(from)[1];
     } else {
-        r.q = *reinterpret_cast<const uint4*>(reinterpret_cast<const uint16_t*>(p) + at);
+        r.q = *reinterpret_cast<const uint4*>(from);
     }
     return r;
 }
@@ -43,30 +50,82 @@ __device__ __forceinline__ Raw8<F32> zero8() {
     return r;
 }
 
+// Keeps packed values packed through a loop: the compiler would convert them before it, twice the registers.
+__device__ __forceinline__ void stay_packed(Raw8<false>& r) { asm volatile("" : "+v"(r.q.x), "+v"(r.q.y), "+v"(r.q.z), "+v"(r.q.w)); }
+
+__device__ __forceinline__ void stay_packed(Raw8<true>&) {}
+// Has the values made here: the compiler would put sums off to the loop's end and keep their terms until then.
+__device__ __forceinline__ void made_here(float (&v)[8]) {
+    asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
+}
+
 // Eight fp32 values rounded once to the row's type.
 template <bool F32>
-__device__ __forceinline__ void store8(void* p, int64_t at, const float (&v)[8]) {
+__device__ __forceinline__ void store8(void* row, uint32_t at, const float (&v)[8]) {
+    char* const to = static_cast<char*>(row) + (size_t)(at * (F32 ? 4u : 2u));
     if constexpr (F32) {
-        float4* f = reinterpret_cast<float4*>(reinterpret_cast<float*>(p) + at);
+        float4* f = reinterpret_cast<float4*>(to);
         f[0] = make_float4(v[0], v[1], v[2], v[3]);
         f[1] = make_float4(v[4], v[5], v[6], v[7]);
     } else {
         bf16x8_t o;
 #pragma unroll
         for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-        *reinterpret_cast<bf16x8_t*>(reinterpret_cast<uint16_t*>(p) + at) = o;
+        *reinterpret_cast<bf16x8_t*>(to) = o;
     }
 }
 
+// A row behind a buffer descriptor (its base has to be the same for a wavefront): lanes behind the row's end read zeros and
+// write nothing, and so do all lanes of an absent row or matrix, without a branch.
+typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+template <bool F32>
+struct RowBuffer {
+    __amdgpu_buffer_rsrc_t rsrc;
+    // row `i` of p [*, H]; there: whether it exists
+    __device__ __forceinline__ RowBuffer(const void* p, int64_t i, int H, bool there) {
+        const int bytes = H * (F32 ? 4 : 2);
+        const bool have = there && p != nullptr;
+        void* const base = have ? const_cast<char*>(static_cast<const char*>(p)) + i * bytes : nullptr;
+        rsrc = __builtin_amdgcn_make_buffer_rsrc(base, (short)0, have ? bytes : 0, 0x00027000);
+    }
+    __device__ __forceinline__ Raw8<F32> load(uint32_t at) const {      // eight values from element `at`, a multiple of 8
+        Raw8<F32> r;
+        if constexpr (F32) {
+            r.q[0] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at * 4, 0, 0));
+            r.q[1] = __builtin_bit_cast(float4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at * 4 + 16, 0, 0));
+        } else {
+            r.q = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(rsrc, at * 2, 0, 0));
+        }
+        return r;
+    }
+    __device__ __forceinline__ void store(uint32_t at, const float (&v)[8]) const {      // rounded once
+        if constexpr (F32) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, make_float4(v[0], v[1], v[2], v[3])), rsrc, at * 4, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, make_float4(v[4], v[5], v[6], v[7])), rsrc, at * 4 + 16, 0, 0);
+        } else {
+            bf16x8_t o;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), rsrc, at * 2, 0, 0);
+        }
+    }
+};
+
 // Sum over the 64 lanes, the same bits in every lane: four steps inside rows of 16 lanes, then the four rows.
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) {
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+// over each 16 lanes, in all of them
+__device__ __forceinline__ float sum_of_16(float v) {
+    v += from_lane<0xb1>(v);       // quad_perm 1 0 3 2
+    v += from_lane<0x4e>(v);       // quad_perm 2 3 0 1
+    v += from_lane<0x141>(v);      // row_half_mirror
+    v += from_lane<0x140>(v);      // row_mirror
+    return v;
+}
 __device__ __forceinline__ float wave_sum(float v) {
-    auto from = [](float x, auto ctrl) {
-        return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), decltype(ctrl)::value, 0xf, 0xf, true));
-    };
-    v += from(v, std::integral_constant<int, 0xb1>{});       // quad_perm 1 0 3 2
-    v += from(v, std::integral_constant<int, 0x4e>{});       // quad_perm 2 3 0 1
-    v += from(v, std::integral_constant<int, 0x141>{});      // row_half_mirror
-    v += from(v, std::integral_constant<int, 0x140>{});      // row_mirror
+    v = sum_of_16(v);
     auto row = [&](int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); };
     return (row(0) + row(16)) + (row(32) + row(48));
 }

@@ -14,7 +14,8 @@ pytestmark = pytest.mark.gpu
 # fp32 operations on the longest path of an output: products and sums of one element (at most 12 each way), a row's sum of H
 # squares (8 to 16 a lane, 6 across lanes, up to 16 wavefronts) halved by the square root; backward goes through two norms.
 FORWARD, BACKWARD = 64, 160
-# of a weight's gradient besides: the rows of a workgroup (here at most 4), up to 1024 / 16 partial sums a thread and 16 threads
+# of a weight's gradient besides: the rows of a workgroup (here at most 9) of up to 16 at a time, up to 4 partial sums a thread, 4 and
+# 16 of these
 WEIGHTS = BACKWARD + 96
 
 
@@ -193,6 +194,20 @@ def test_rows_of_zeros_large_and_small_values_and_saturated_gates():
     assert (ro[0] == 0).all() and (n[0] == 0).all()
     got = _run_backward(x, False, B.ALST_FLAG_DW_FP32)
     with np.errstate(over="ignore"):
+        _check_backward(x, got)
+
+
+def test_infinite_gates_close_and_open():
+    N, H = 6, 200
+    for gate in ("row", "element"):
+        x = _inputs(N, H, True, gate, True, True)
+        x["gate"][0], x["gate"][1] = float("-inf"), float("inf")
+        ro, n = _run_forward(x, True)
+        got = _run_backward(x, True)
+        assert torch.equal(ro[0].cpu(), x["r"][0]) and (got["d_branch"][0] == 0).all()
+        assert (got["d_gate"][:2] == 0).all()
+        x["gate"][0], x["gate"][1] = -200, 200          # as far as fp32 tells
+        _check_forward(x, ro, n)
         _check_backward(x, got)
 
 
