@@ -25,8 +25,8 @@ extern "C" {
 #endif
 
 /* Bytes of device scratch that alst_embedding_backward needs, 0 if the shape is invalid.  Pure host
- * arithmetic.  It grows with N (the tokens in sorted order, 16 N bytes, and fp32 sums of the rows of a token
- * whose run is cut, at most N H / 2 bytes) and not with V but for V / 8 bytes; a workspace serves every N up
+ * arithmetic.  Large terms: 16 N bytes for the tokens in sorted order, V bytes for the tokens that occur, and fp32 sums of tokens
+ * whose sorted rows are cut into ranges: N H / 8 bytes, in short calls up to N H and 32 MB.  A workspace serves every N up
  * to its own. */
 size_t alst_embedding_workspace_bytes(int64_t N, int64_t H, int64_t V);
 

@@ -44,10 +44,10 @@ def test_workspace_sizes(lib):
     size = B.alst_embedding_workspace_bytes
     assert size(0, 64, 10) == size(1, 0, 10) == size(1, 64, 0) == size(2 ** 30 + 1, 64, 10) == size(1, 64, 2 ** 24 + 1) == 0
     assert size(1, 2 ** 20 + 8, 10) == 0
-    # the sorted order and a share of the rows; next to nothing for the vocabulary
+    # the sorted order, a share of the rows and a mark a token
     N, H, V = 131072, 4096, 128256
-    assert 16 * N < size(N, H, V) <= 16 * N + N * H // 2 + V // 8 + (1 << 20)
-    for n in (1, 100, 4097, N):         # a workspace serves shorter calls
+    assert 16 * N < size(N, H, V) <= 16 * N + N * H // 8 + V + (2 << 20)
+    for n in (1, 100, 4096, 4097, 8191, 8192, 16383, 16384, 32767, 32768, N):         # a workspace serves shorter calls
         assert size(n, H, V) <= size(n + 1, H, V) <= size(N + 1, H, V)
     norm = B.alst_block_norm_workspace_bytes
     assert norm(0, 64) == norm(1, 0) == norm(5, 16392) == 0
