@@ -91,6 +91,52 @@ def test_backward(N, H, V, law):
     assert status == B.ALST_OK
 
 
+def _by_lengths(lengths, seed=0):
+    """Tokens 1, 3, 5, ... with these numbers of rows, in random order."""
+    t = np.repeat(np.arange(len(lengths)) * 2 + 1, lengths).astype(np.int32)
+    np.random.default_rng(seed).shuffle(t)
+    return t, 2 * len(lengths) + 2
+
+
+@pytest.mark.parametrize("run,rows", [(8, 2000), (16, 70000), (128, 600000)])
+@pytest.mark.parametrize("first", [0, 1, 5])
+def test_tokens_whose_rows_end_at_and_beside_the_ranges_of_the_sums(run, rows, first):
+    """Sorted rows are added up in ranges of 8 rows in short calls and of 128 in long ones (at 8 columns): tokens that fill a range, end
+    or begin with one, lie in two, and go through one, two and many."""
+    some = [first, run - first, run, run, 2 * run, run - 1, 1, run + 1, run - 1, 1, 2 * run - 1, 1, 3 * run, run // 2, run, run // 2,
+            run // 2, 2 * run, run // 2, run // 2, 4 * run + 3, run - 3, 9 * run + 1, run - 1, 20 * run, 2, run - 2, 1]
+    some = [n for n in some if n]
+    lengths = some * (rows // sum(some)) + [rows % sum(some) + 1]
+    t, V = _by_lengths(lengths)
+    assert len(t) in (rows, rows + 1)
+    g = torch.Generator().manual_seed(run)
+    dy = U.bf16((len(t), 8), g)
+    got, _ = _backward(t, dy, V, flags=B.ALST_FLAG_DW_FP32)
+    index = torch.from_numpy(t).long()
+    want = torch.zeros((V, 8), dtype=torch.float64).index_add_(0, index, dy.double()).numpy()
+    mag = torch.zeros((V, 8), dtype=torch.float64).index_add_(0, index, dy.double().abs()).numpy()
+    U.check("dE", got, want, mag, np.bincount(t, minlength=V)[:, None] + 2.0)
+
+
+@pytest.mark.parametrize("N,H,V", [(600001, 8, 70000), (1 << 20, 8, 300), ((1 << 20) + 1, 8, 300), (59000, 4104, 900)])
+@pytest.mark.parametrize("law", ["zipf", "same", "two"])
+def test_backward_of_long_calls(N, H, V, law):
+    """Long ranges, shares of the sort above 4096 rows (from 2^20 rows on), more than 512 columns times 8."""
+    if H > 8 and law == "two":
+        pytest.skip("the others cover it")
+    t = _tokens(law, N, V, 5)
+    dy = U.bf16((N, H), torch.Generator().manual_seed(N))
+    got, status = _backward(t, dy, V, flags=B.ALST_FLAG_DW_FP32)
+    keep = torch.from_numpy(t != IGN)
+    index = torch.from_numpy(t)[keep].long()
+    want = torch.zeros((V, H), dtype=torch.float64).index_add_(0, index, dy[keep].double())
+    mag = torch.zeros((V, H), dtype=torch.float64).index_add_(0, index, dy[keep].double().abs())
+    rows = np.bincount(t[t != IGN], minlength=V)[:, None]
+    # 128 rows of a range, the partial sums of a wavefront (an eighth of a token's ranges), eight wavefronts, scale
+    U.check("dE", got, U.to64(want), U.to64(mag), np.minimum(rows, 128 + rows / 1024 + 8) + 2.0)
+    assert status == B.ALST_OK
+
+
 @pytest.mark.parametrize("V", [(1 << 18) - 1, 1 << 18, 1 << 20, 1 << 24])
 def test_backward_of_large_vocabularies(V):
     """The number of the sort's passes changes at 2^18 tokens and at 2^27."""
