@@ -118,12 +118,13 @@ def test_tokens_whose_rows_end_at_and_beside_the_ranges_of_the_sums(run, rows, f
     U.check("dE", got, want, mag, np.bincount(t, minlength=V)[:, None] + 2.0)
 
 
-@pytest.mark.parametrize("N,H,V", [(600001, 8, 70000), (1 << 20, 8, 300), ((1 << 20) + 1, 8, 300), (59000, 4104, 900)])
-@pytest.mark.parametrize("law", ["zipf", "same", "two"])
+LONG = [(600001, 8, 70000), (1 << 20, 8, 300), ((1 << 20) + 1, 8, 300)]
+
+
+@pytest.mark.parametrize("N,H,V,law", [(*s, law) for s in LONG for law in ("zipf", "same", "two")] +
+                         [(59000, 4104, 900, law) for law in ("zipf", "same")])
 def test_backward_of_long_calls(N, H, V, law):
     """Long ranges, shares of the sort above 4096 rows (from 2^20 rows on), more than 512 columns times 8."""
-    if H > 8 and law == "two":
-        pytest.skip("the others cover it")
     t = _tokens(law, N, V, 5)
     dy = U.bf16((N, H), torch.Generator().manual_seed(N))
     got, status = _backward(t, dy, V, flags=B.ALST_FLAG_DW_FP32)
