@@ -171,12 +171,14 @@ def alst_tiled_ce_workspace_bytes(N: int, H: int, V: int, tile: int, flags: int 
 
 
 def _ptr(t):
-    return None if t is None else ctypes.c_void_p(t.data_ptr())
+    return None if t is None else t.data_ptr()
 
 
 def _want(t, name: str, dtype, shape=None, optional: bool = False):
     """The C ABI sees only addresses: a tensor of another dtype, a strided view or a host tensor
     would be reinterpreted silently, so the binding refuses them here."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and (shape is None or t.shape == shape) and t.is_contiguous():
+        return
     if t is None and optional:
         return
     why = None
@@ -417,11 +419,16 @@ def _call(where: str, tensors: dict, *args) -> None:
     """Calls an entry point on the current stream of the device that all `tensors` are on (and only there: another
     device may be the current one).  The last check of a wrapper, like _on_device."""
     _on_device(**tensors)
-    devices = {t.device for t in tensors.values() if t is not None}
+    devices = {t.get_device() for t in tensors.values() if t is not None}
     if len(devices) != 1:
-        raise TypeError(f"{where}: tensors on different devices: {sorted(str(d) for d in devices)}")
-    with torch.cuda.device(devices.pop()):
-        st = getattr(load_library(), where)(*args, _stream())
+        raise TypeError(f"{where}: tensors on different devices: {sorted(devices)}")
+    device = devices.pop()
+    entry = getattr(load_library(), where)
+    if device == torch.cuda.current_device():
+        st = entry(*args, _stream())
+    else:
+        with torch.cuda.device(device):
+            st = entry(*args, _stream())
     _check(st, where)
 
 

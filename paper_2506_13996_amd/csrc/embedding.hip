@@ -7,7 +7,7 @@
 // Rows of tokens that do not occur are filled with zeros beside the steps that leave the memory idle.
 //
 // Both are bound by HBM.  131072 rows of 4096 by Zipf-distributed tokens: lookup 245 us = 5.1 TB/s.  Their gradient over 128256 tokens
-// 430 us = 4.9 TB/s: 36 us of sort, 290 us of sums (1.07 GB of rows in the tokens' order, which come at 4.5 TB/s; rows in the order
+// 458 us = 4.6 TB/s: 36 us of sort, 290 us of sums (1.07 GB of rows in the tokens' order, which come at 4.5 TB/s; rows in the order
 // of memory at 5.5), the rest zeros (at 6 TB/s).
 #include <algorithm>
 
