@@ -46,7 +46,8 @@ size_t alst_block_norm_workspace_bytes(int64_t N, int64_t H);
  *   residual      [N,H]
  *   branch        [N,H] or NULL: then w_post, gate and residual_out are NULL and w_pre is not
  *   w_post        [H] or NULL: the block's output is not normalised
- *   gate          [N,H] (gate_cols = H), [N] (gate_cols = 1) or NULL (gate_cols = 0)
+ *   gate          [N,H] (gate_cols = H), [N] (gate_cols = 1; it and d_gate need no alignment beyond their elements') or NULL
+ *                 (gate_cols = 0)
  *   w_pre         [H] or NULL: then normed is NULL
  *   residual_out  [N,H] r', overwritten; may be `residual` itself, or `branch` if both are of the same type
  *   normed        [N,H] n, overwritten; may be `branch` itself

@@ -10,7 +10,7 @@
  *
  * A token equal to `ignore_index` (padding) has a row of zeros and takes no part in dE: its row of dy is not
  * read.  Conventions are those of alst.h: device pointers, dense row-major without strides, H a multiple of 8,
- * 16-byte aligned base pointers (tokens too), the caller owns every buffer, calls validate on the host, enqueue
+ * 16-byte aligned base pointers (tokens: 4 bytes), the caller owns every buffer, calls validate on the host, enqueue
  * on `stream` and return an alst_status without synchronising; they allocate nothing and can be captured into
  * a HIP graph.  1 <= N <= 2^30, 8 <= H <= 2^20, 1 <= V <= 2^24.  No output may overlap another buffer.
  * A token that is neither ignore_index nor in [0,V) is treated as ignored and reported in a status word.

@@ -388,10 +388,12 @@ static int validate_norm(const NormParams& p, int64_t H, int64_t gate_cols) {
     if (!norm_shape_ok(p.N, H)) return ALST_ERR_SHAPE;
     if (p.gate ? gate_cols != 1 && gate_cols != H : gate_cols != 0) return ALST_ERR_SHAPE;
     if (H % 8 != 0) return ALST_ERR_ALIGN;
-    const void* ptrs[] = {p.residual, p.d_residual_out, p.branch, p.w_post, p.gate, p.w_pre, p.d_normed, p.residual_out, p.d_residual,
-                          p.normed, p.d_branch, p.d_gate, p.parts};
+    const void* ptrs[] = {p.residual, p.d_residual_out, p.branch, p.w_post, p.w_pre, p.d_normed, p.residual_out, p.d_residual, p.normed,
+                          p.d_branch, p.parts};
     for (const void* q : ptrs)
         if (!aligned_to(q, 16)) return ALST_ERR_ALIGN;
+    const uintptr_t gate = gate_cols == 1 ? 2 : 16;      // (a gate of one logit a row is read by elements)
+    if (!aligned_to(p.gate, gate) || !aligned_to(p.d_gate, gate)) return ALST_ERR_ALIGN;
     if (!(p.eps >= 1.17549435e-38f) || !(p.eps <= 3.402823466e38f)) return ALST_ERR_UNSUPPORTED;
     return ALST_OK;
 }

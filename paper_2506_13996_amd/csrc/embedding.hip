@@ -497,7 +497,7 @@ int alst_embedding_forward(const int32_t* tokens, const void* E, int64_t N, int6
     if (!tokens || !E || !y) return ALST_ERR_NULL;
     if (flags & ~ALST_FLAG_RESIDUAL_FP32) return ALST_ERR_UNSUPPORTED;
     if (!embedding_shape_ok(N, H, V)) return ALST_ERR_SHAPE;
-    if (H % 8 != 0 || !aligned_to(tokens, 16) || !aligned_to(E, 16) || !aligned_to(y, 16) || !aligned_to(device_status_out, 4))
+    if (H % 8 != 0 || !aligned_to(tokens, 4) || !aligned_to(E, 16) || !aligned_to(y, 16) || !aligned_to(device_status_out, 4))
         return ALST_ERR_ALIGN;
     const int W = (int)std::min<int64_t>((H + kForwardColumns - 1) / kForwardColumns, 4), R = 4 / W;
     // a row a wavefront at a time (131072 x 4096: 245 us, 262 with four); of short rows four, or the launch waits for tokens
@@ -518,7 +518,7 @@ int alst_embedding_backward(const int32_t* tokens, const void* dy, int64_t N, in
     if (!tokens || !dy || !dE || !workspace) return ALST_ERR_NULL;
     if (flags & ~(ALST_FLAG_RESIDUAL_FP32 | ALST_FLAG_DW_FP32 | ALST_FLAG_DW_ACCUMULATE)) return ALST_ERR_UNSUPPORTED;
     if (!embedding_shape_ok(N, H, V)) return ALST_ERR_SHAPE;
-    if (H % 8 != 0 || !aligned_to(tokens, 16) || !aligned_to(dy, 16) || !aligned_to(dE, 16) || !aligned_to(workspace, 16))
+    if (H % 8 != 0 || !aligned_to(tokens, 4) || !aligned_to(dy, 16) || !aligned_to(dE, 16) || !aligned_to(workspace, 16))
         return ALST_ERR_ALIGN;
     const EmbeddingLayout L = make_embedding_layout(N, H, V);
     if (workspace_bytes < L.total) return ALST_ERR_WORKSPACE;

@@ -212,6 +212,20 @@ def test_backward_gives_the_same_bits_every_time_and_on_another_stream():
     assert torch.equal(first, third)
 
 
+def test_tokens_at_any_offset_of_a_batch():
+    N, H, V = 333, 64, 50
+    g = torch.Generator().manual_seed(8)
+    batch = torch.from_numpy(np.random.default_rng(8).integers(0, V, (4, N)).astype(np.int32))
+    E, dy, d = U.bf16((V, H), g), U.bf16((N, H), g), batch.cuda()
+    ws = B.alloc_embedding_workspace(N, H, V)
+    for k in range(4):
+        y, dE = U.Guarded((N, H), torch.bfloat16), U.Guarded((V, H), torch.bfloat16)
+        B.alst_embedding_forward(d[k], E.cuda(), y=y.t)
+        B.alst_embedding_backward(d[k], dy.cuda(), dE=dE.t, workspace=ws)
+        assert torch.equal(y.t.cpu(), E[batch[k].long()]) and y.intact() and dE.intact()
+        _check_backward(dE.t, batch[k].numpy(), dy, V)
+
+
 def test_captured_calls_follow_their_inputs():
     N, H, V = 700, 72, 90
     g = torch.Generator().manual_seed(4)

@@ -62,14 +62,14 @@ def test_embedding_refusals(lib):
         return lib.alst_embedding_forward(vp(tokens), vp(E), N, H, V, -100, 1.0, vp(y), vp(status), flags, None)
     assert fwd(tokens=None) == fwd(E=None) == fwd(y=None) == B.ALST_ERR_NULL
     assert fwd(N=0) == fwd(H=0) == fwd(V=0) == fwd(V=2 ** 24 + 1) == fwd(N=2 ** 30 + 1) == fwd(H=2 ** 20 + 8) == B.ALST_ERR_SHAPE
-    assert fwd(H=60) == fwd(E=0x2008) == fwd(y=0x3002) == fwd(tokens=0x1004) == fwd(status=0x4002) == B.ALST_ERR_ALIGN
+    assert fwd(H=60) == fwd(E=0x2008) == fwd(y=0x3002) == fwd(tokens=0x1002) == fwd(status=0x4002) == B.ALST_ERR_ALIGN
     assert fwd(flags=B.ALST_FLAG_DW_FP32) == fwd(flags=64) == B.ALST_ERR_UNSUPPORTED
 
     def bwd(tokens=0x1000, dy=0x2000, N=4, H=64, V=10, dE=0x3000, ws=0x4000, wsb=1 << 40, flags=0):
         return lib.alst_embedding_backward(vp(tokens), vp(dy), N, H, V, -100, 1.0, vp(dE), vp(ws), wsb, flags, None)
     assert bwd(tokens=None) == bwd(dy=None) == bwd(dE=None) == bwd(ws=None) == B.ALST_ERR_NULL
     assert bwd(N=0) == bwd(V=-1) == B.ALST_ERR_SHAPE
-    assert bwd(H=4) == bwd(dy=0x2004) == bwd(dE=0x3008) == bwd(ws=0x4008) == B.ALST_ERR_ALIGN
+    assert bwd(H=4) == bwd(dy=0x2004) == bwd(dE=0x3008) == bwd(ws=0x4008) == bwd(tokens=0x1002) == B.ALST_ERR_ALIGN
     assert bwd(flags=B.ALST_FLAG_REDUCE_SUM) == bwd(flags=B.ALST_FLAG_FORWARD_ONLY) == B.ALST_ERR_UNSUPPORTED
     assert bwd(wsb=B.alst_embedding_workspace_bytes(4, 64, 10) - 1) == B.ALST_ERR_WORKSPACE
 
@@ -83,7 +83,7 @@ def test_block_norm_refusals(lib):
     assert fwd(b=None, w1=None, ro=None, z=0x7000, cols=1) == fwd(b=None, w1=None, ro=None, w2=None, n=None) == B.ALST_ERR_NULL
     assert fwd(N=0) == fwd(H=0) == fwd(H=16392) == fwd(N=2 ** 30 + 1) == B.ALST_ERR_SHAPE
     assert fwd(z=0x7000) == fwd(z=0x7000, cols=2) == fwd(cols=64) == fwd(cols=1) == B.ALST_ERR_SHAPE
-    assert fwd(H=60) == fwd(r=0x1004) == fwd(w1=0x3002) == fwd(n=0x6008) == fwd(z=0x7002, cols=1) == B.ALST_ERR_ALIGN
+    assert fwd(H=60) == fwd(r=0x1004) == fwd(w1=0x3002) == fwd(n=0x6008) == fwd(z=0x7001, cols=1) == fwd(z=0x7002, cols=64) == B.ALST_ERR_ALIGN
     for eps in (0.0, -1e-6, 1e-40, float("nan"), float("inf")):
         assert fwd(eps=eps) == B.ALST_ERR_UNSUPPORTED
     assert fwd(flags=B.ALST_FLAG_DW_FP32) == fwd(flags=1 << 9) == B.ALST_ERR_UNSUPPORTED
