@@ -32,13 +32,16 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(const int32_t* _
     for (int64_t g0 = blockIdx.x * rows; g0 < N; g0 += gridDim.x * rows) {
         const int64_t i0 = g0 + __builtin_amdgcn_readfirstlane(threadIdx.y) * ROWS;
         Raw8<false> r[ROWS][2];
+        float factor[ROWS];                              // (0 for a row of zeros, whatever scale is)
 #pragma unroll
         for (int j = 0; j < ROWS; ++j) {
             const int64_t i = i0 + j;
             const int t = __builtin_amdgcn_readfirstlane(i < N ? tokens[i] : ignore_index);
             const bool named = t >= 0 && t < V;
             if (!named && t != ignore_index && status && threadIdx.x == 0 && blockIdx.y == 0) *status = ALST_ERR_LABEL_RANGE;
-            const RowBuffer<false> row(E, t, H, named && t != ignore_index);
+            const bool kept = named && t != ignore_index;
+            const RowBuffer<false> row(E, t, H, kept);
+            factor[j] = kept ? scale : 0.f;
             r[j][0] = row.load(col);
             r[j][1] = row.load(col + next);
         }
@@ -49,7 +52,7 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(const int32_t* _
             for (int c = 0; c < 2; ++c) {
                 float v[8];
 #pragma unroll
-                for (int k = 0; k < 8; ++k) v[k] = r[j][c].get(k) * scale;
+                for (int k = 0; k < 8; ++k) v[k] = r[j][c].get(k) * factor[j];
                 row.store(col + c * next, v);
             }
         }

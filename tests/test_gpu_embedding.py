@@ -75,6 +75,9 @@ def test_forward_reports_tokens_out_of_range_and_gives_them_zeros():
         B.alst_embedding_forward(t, E, y=y.t, device_status_out=status)
         assert int(status) == B.ALST_ERR_LABEL_RANGE
         assert y.t[:, 0].tolist() == [1, 0, 0, 1] and y.intact()
+    # rows of zeros do not go by the scale
+    B.alst_embedding_forward(torch.tensor([3, IGN, 1, IGN], dtype=torch.int32, device="cuda"), E, float("inf"), y=y.t)
+    assert y.t[:, 0].tolist() == [float("inf"), 0, float("inf"), 0]
     # an ignore_index inside the vocabulary
     B.alst_embedding_forward(torch.tensor([3, 0, 3, 0], dtype=torch.int32, device="cuda"), E, 1.0, 3, y=y.t)
     assert y.t[:, 0].tolist() == [0, 1, 0, 1]

@@ -126,6 +126,15 @@ def test_grads_refusals(lib):
     assert norm(ts(), wsb=short) == both(ts(), wsb=short) == B.ALST_ERR_WORKSPACE
 
 
+def test_the_tiled_operators_refuse_an_fp32_stream(lib):
+    f = B.ALST_FLAG_RESIDUAL_FP32
+    assert lib.alst_tiled_ce_forward(vp(0x1000), vp(0x2000), vp(0x3000), 16, 64, 32, 8, -100, vp(0x4000), None, None, vp(0x5000), 1 << 40, f,
+                                     None) == B.ALST_ERR_UNSUPPORTED
+    assert lib.alst_tiled_mlp_forward(vp(0x1000), vp(0x2000), vp(0x3000), vp(0x4000), 16, 64, 64, 8, vp(0x5000), vp(0x6000), 1 << 40, f,
+                                      None) == B.ALST_ERR_UNSUPPORTED
+    assert lib.alst_tiled_linear_forward(vp(0x1000), vp(0x2000), 16, 64, 64, 8, vp(0x5000), None, 0, f, None) == B.ALST_ERR_UNSUPPORTED
+
+
 def test_binding_refuses_tensors_the_abi_would_reinterpret():
     N, H, V = 4, 16, 10
     bf = lambda *sh: torch.zeros(sh, dtype=torch.bfloat16)  # noqa: E731
