@@ -7,7 +7,7 @@
 // Rows of tokens that do not occur are filled with zeros beside the steps that leave the memory idle.
 //
 // Both are bound by HBM.  131072 rows of 4096 by Zipf-distributed tokens: lookup 245 us = 5.1 TB/s.  Their gradient over 128256 tokens
-// 458 us = 4.6 TB/s: 36 us of sort, 290 us of sums (1.07 GB of rows in the tokens' order, which come at 4.5 TB/s; rows in the order
+// 459 us = 4.6 TB/s: 36 us of sort, 300 us of sums (1.07 GB of rows in the tokens' order, which come at 4.5 TB/s; rows in the order
 // of memory at 5.5), the rest zeros (at 6 TB/s).
 #include <algorithm>
 
@@ -22,7 +22,8 @@ namespace alst {
 constexpr int64_t kMostGroups = 1 << 22;        // workgroups of a launch (their threads have to stay below 2^32); more work is walked
 
 constexpr int kForwardColumns = 1024;          // of a wavefront: two groups of eight values a lane
-// W wavefronts (blockDim.x / 64) take ROWS rows, 1024 columns each; the R rows of wavefronts of a workgroup lie behind each other.  A token that takes no part has no row: it is read as zeros.
+// W wavefronts (blockDim.x / 64) take ROWS rows, 1024 columns each; the R rows of wavefronts of a workgroup lie behind each other.
+// A token that takes no part has no row: it is read as zeros.
 template <bool F32, int ROWS>
 __global__ __launch_bounds__(256) void embedding_forward_kernel(const int32_t* __restrict__ tokens, const uint16_t* __restrict__ E,
                                                                 void* __restrict__ y, int64_t N, int H, int V, int ignore_index,
@@ -277,32 +278,41 @@ __global__ __launch_bounds__(kSortThreads) void sort_short_kernel(SortSource src
 struct Grad {
     void* dE;
     float scale;
+    bool f32, accumulate;
 };
 
-// dE's row of a token, from the sum of its rows.  OLD: what the row held, where the sums are added to it.
-template <bool SUM32, bool ACCUMULATE>
-__device__ __forceinline__ void write_grad(const Grad& g, int key, int H, uint32_t col, const float (&sum)[8], const Raw8<SUM32>& old) {
+template <bool F32>
+__device__ __forceinline__ void write_grad_as(const Grad& g, int key, int H, uint32_t col, const float (&sum)[8]) {
+    const RowBuffer<F32> row(g.dE, key, H, true);
     float v[8];
 #pragma unroll
-    for (int k = 0; k < 8; ++k) v[k] = ACCUMULATE ? old.get(k) + sum[k] * g.scale : sum[k] * g.scale;
-    RowBuffer<SUM32>(g.dE, key, H, true).store(col, v);
+    for (int k = 0; k < 8; ++k) v[k] = sum[k] * g.scale;
+    if (g.accumulate) {
+        const Raw8<F32> old = row.load(col);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) v[k] += old.get(k);
+    }
+    row.store(col, v);
+}
+__device__ __forceinline__ void write_grad(const Grad& g, int key, int H, uint32_t col, const float (&sum)[8]) {
+    if (g.f32) write_grad_as<true>(g, key, H, col, sum);
+    else write_grad_as<false>(g, key, H, col, sum);
 }
 
 constexpr int kSumThreads = 512;
-template <bool F32, bool ACCUMULATE> constexpr int kRowsTogether = F32 || ACCUMULATE ? 8 : 16;               // rows of dy that a wavefront has in flight
+template <bool F32> constexpr int kRowsTogether = F32 ? 8 : 16;               // rows of dy that a wavefront has in flight
 constexpr int kJoinThreads = 512;
 constexpr int kJoinGroups = 256;               // workgroups of the joins' launch for each 512 columns, which walk the list
 
 // A range is `run` sorted rows.  Its wavefronts add up the tokens that begin in it, and follow the last one into the next range.
 // Only a token that goes through a whole range besides is cut: parts[range][1] has its rows of the range where it begins, which is
 // then listed, parts[range][0] those of the ranges behind.  A workgroup: a range and 512 columns a wavefront; workgroups from
-// `ranges` on: rows of zeros.  Rows of dE that are added to are asked for with the rows that end their tokens (16384 x 5120, fp32 sums:
-// 117 us, 129 when each was waited for).
-template <bool F32, bool SUM32, bool ACCUMULATE>
+// `ranges` on: rows of zeros.
+template <bool F32>
 __global__ __launch_bounds__(kSumThreads) void run_sums_kernel(const Pair* __restrict__ pairs, const void* __restrict__ dy, int64_t N,
                                                                int H, int V, int run, int64_t ranges, float* __restrict__ parts,
                                                                Pair* __restrict__ list, EmbeddingHeader* header, Grad g, ZeroRows zeros) {
-    constexpr int kTogether = kRowsTogether<F32, ACCUMULATE>;
+    constexpr int kTogether = kRowsTogether<F32>;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
     const int64_t range = blockIdx.x, p0 = range * run;
     if (range >= ranges) {
@@ -335,13 +345,10 @@ __global__ __launch_bounds__(kSumThreads) void run_sums_kernel(const Pair* __res
         const int follows = b0 + 64 < stop ? key_at(b0 + 64) : -1;
         for (int j0 = 0; j0 < here; j0 += kTogether) {
             Raw8<F32> r[kTogether];
-            Raw8<SUM32> old[kTogether];
-            auto behind = [&](int at) { return at + 1 == here ? follows : __builtin_amdgcn_readlane(mine.key, (at + 1) & 63); };
 #pragma unroll
             for (int j = 0; j < kTogether; ++j) {
                 const int key = __builtin_amdgcn_readlane(mine.key, j0 + j), row = __builtin_amdgcn_readlane(mine.row, j0 + j);
                 r[j] = RowBuffer<F32>(dy, row, H, key < V).load(col);
-                if (ACCUMULATE) old[j] = RowBuffer<SUM32>(g.dE, key, H, key < V && key != behind(j0 + j)).load(col);
             }
 #pragma unroll
             for (int j = 0; j < kTogether; ++j) {
@@ -350,14 +357,14 @@ __global__ __launch_bounds__(kSumThreads) void run_sums_kernel(const Pair* __res
                 if (key >= V) return;                    // (no rows behind the last token's, or behind `stop`)
 #pragma unroll
                 for (int k = 0; k < 8; ++k) sum[k] += r[j].get(k);
-                if (key == behind(at)) continue;
+                if (key == (at + 1 == here ? follows : __builtin_amdgcn_readlane(mine.key, (at + 1) & 63))) continue;
                 if (head) {
                     RowBuffer<true>(parts, range * 2, H, true).store(col, sum);
                 } else if (tail_cut && b0 + at + 1 == stop) {
                     RowBuffer<true>(parts, range * 2 + 1, H, true).store(col, sum);
                     if (blockIdx.y == 0 && threadIdx.x == 0) list[atomicAdd(&header->joins, 1)] = {key, (int32_t)range};
                 } else {
-                    write_grad<SUM32, ACCUMULATE>(g, key, H, col, sum, old[j]);
+                    write_grad(g, key, H, col, sum);
                 }
                 head = false;
 #pragma unroll
@@ -370,7 +377,6 @@ __global__ __launch_bounds__(kSumThreads) void run_sums_kernel(const Pair* __res
 // The tokens that were cut: the partial sums of the range where one begins (slot 1) and of those behind it (slot 0), dealt to the
 // wavefronts of the workgroup in turn.  The list's order changes nothing: each token has its own row.  The first `groups` workgroups
 // walk the list, 512 columns each, and wait for memory most of their time (18 us); the others fill rows with zeros beside them.
-template <bool SUM32, bool ACCUMULATE>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Pair* __restrict__ pairs, int64_t N, int H, int run, int64_t ranges,
                                                             int slabs, int groups, const Pair* __restrict__ list,
                                                             const EmbeddingHeader* __restrict__ header, const float* __restrict__ parts,
@@ -422,7 +428,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Pair* __restri
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum[j] += r.get(j);
             }
-            write_grad<SUM32, ACCUMULATE>(g, key, H, col, sum, RowBuffer<SUM32>(g.dE, key, H, ACCUMULATE).load(col));
+            write_grad(g, key, H, col, sum);
         }
         __syncthreads();
     }
@@ -529,16 +535,15 @@ int alst_embedding_backward(const int32_t* tokens, const void* dy, int64_t N, in
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     EmbeddingHeader* const header = reinterpret_cast<EmbeddingHeader*>(ws);
     float* const parts = reinterpret_cast<float*>(ws + L.parts);
-    const Grad g = {dE, scale};
-    const bool rows32 = flags & ALST_FLAG_RESIDUAL_FP32, sums32 = flags & ALST_FLAG_DW_FP32, accumulate = flags & ALST_FLAG_DW_ACCUMULATE;
-    uint8_t* const occurs = accumulate ? nullptr : ws + L.occurs;
+    const Grad g = {dE, scale, (flags & ALST_FLAG_DW_FP32) != 0, (flags & ALST_FLAG_DW_ACCUMULATE) != 0};
+    uint8_t* const occurs = g.accumulate ? nullptr : ws + L.occurs;
     // rows of zeros: a share beside each step of the sort (whose few workgroups leave the memory idle for about that many bytes'
     // time), the rest beside the sums
-    const int64_t row_bytes = H * (sums32 ? 4 : 2);
+    const int64_t row_bytes = H * (g.f32 ? 4 : 2);
     ZeroRows zeros = {dE, occurs, 0, 0, (int)(row_bytes / 2)};
     auto take_zeros = [&](int64_t bytes) {               // workgroups of 16 wavefronts that fill the next `bytes`
         zeros.from = zeros.upto;
-        if (accumulate || bytes == 0) return 0;
+        if (g.accumulate || bytes == 0) return 0;
         zeros.upto = std::min<int64_t>(V, zeros.from + (bytes + row_bytes - 1) / row_bytes);
         return (int)std::min<int64_t>(zeros.groups(), 2048);
     };
@@ -575,19 +580,12 @@ int alst_embedding_backward(const int32_t* tokens, const void* dy, int64_t N, in
     take_zeros(join ? std::max<int64_t>(left - kZerosBesideJoins, 0) : left);
     const int64_t fill = std::min((zeros.groups() + columns - 1) / columns, kMostGroups);
     Pair* const list = reinterpret_cast<Pair*>(ws + L.list);
-    using Sums = void (*)(const Pair*, const void*, int64_t, int, int, int, int64_t, float*, Pair*, EmbeddingHeader*, Grad, ZeroRows);
-    static const Sums kernels[2][2][2] = {{{run_sums_kernel<false, false, false>, run_sums_kernel<false, false, true>},
-                                           {run_sums_kernel<false, true, false>, run_sums_kernel<false, true, true>}},
-                                          {{run_sums_kernel<true, false, false>, run_sums_kernel<true, false, true>},
-                                           {run_sums_kernel<true, true, false>, run_sums_kernel<true, true, true>}}};
-    const Sums sums = kernels[rows32][sums32][accumulate];
+    auto sums = flags & ALST_FLAG_RESIDUAL_FP32 ? run_sums_kernel<true> : run_sums_kernel<false>;
     hipLaunchKernelGGL(sums, dim3((unsigned)(L.ranges + fill), (unsigned)columns), dim3(waves * 64), 0, s, src.pairs, dy, N, (int)H, (int)V,
                        L.run, L.ranges, parts, list, header, g, zeros);
     if (join) {
         const int fill_join = take_zeros(left), groups = (int)std::min<int64_t>(L.ranges / 2, kJoinGroups) * slabs;
-        auto joins = sums32 ? (accumulate ? join_kernel<true, true> : join_kernel<true, false>)
-                            : (accumulate ? join_kernel<false, true> : join_kernel<false, false>);
-        hipLaunchKernelGGL(joins, dim3(groups + fill_join), dim3(kJoinThreads), 0, s, src.pairs, N, (int)H, L.run, L.ranges, slabs, groups,
+        hipLaunchKernelGGL(join_kernel, dim3(groups + fill_join), dim3(kJoinThreads), 0, s, src.pairs, N, (int)H, L.run, L.ranges, slabs, groups,
                            (const Pair*)list, (const EmbeddingHeader*)header, (const float*)parts, g, zeros);
     }
     return hipGetLastError() == hipSuccess ? ALST_OK : ALST_ERR_HIP;
