@@ -4,6 +4,8 @@ global norm; against the same step differentiated in 64 bits on the CPU.
 
 Bar: 2e-2 of the largest gradient, that of the library's other parity tests.  Between the parameters and a gradient there are about 20
 roundings to bf16 (half a step of 2^-9 of the value each, independent): 20 ** 0.5 * 2^-9 * 0.6 = 5e-3 of a typical value."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -147,3 +149,34 @@ def test_a_captured_step_follows_its_tokens():
         s.run()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(replayed, s.results()))
+
+
+def test_two_threads_with_streams_and_workspaces_of_their_own():
+    steps = [Step(600, 128, 192, 700, seed=5), Step(350, 264, 96, 3000, seed=6)]
+    want = []
+    for s in steps:
+        s.run()
+        torch.cuda.synchronize()
+        want.append([t.clone() for t in s.results()])
+        for t in s.results():
+            t.zero_()
+    torch.cuda.synchronize()
+    failed = []
+
+    def work(s):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(3):
+                    s.run()
+                torch.cuda.current_stream().synchronize()
+        except Exception as e:      # (a thread's exception would be lost)
+            failed.append(e)
+
+    threads = [threading.Thread(target=work, args=(s,)) for s in steps]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not failed, failed
+    for s, w in zip(steps, want):
+        assert all(torch.equal(a, b) for a, b in zip(s.results(), w))
