@@ -92,7 +92,7 @@ struct Columns {
 
 // DENSE: a gate for each element.  Absent matrices read as zeros, absent weights as ones: the arithmetic has no branches.
 template <bool F32, bool DENSE, int VPT>
-__global__ __launch_bounds__(VPT == 1 ? 1024 : 512) void norm_forward_kernel(NormParams p) {
+__global__ __launch_bounds__(512) void norm_forward_kernel(NormParams p) {
     extern __shared__ float lds[];
     RowPlace at(lds);
     const Columns<VPT> col(at);
@@ -157,7 +157,7 @@ __global__ __launch_bounds__(VPT == 1 ? 1024 : 512) void norm_forward_kernel(Nor
 }
 
 template <bool F32, bool DENSE, int VPT>
-__global__ __launch_bounds__(VPT == 1 ? 1024 : 512) void norm_backward_kernel(NormParams p) {
+__global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
     extern __shared__ float lds[];
     RowPlace at(lds);
     const Columns<VPT> col(at);
@@ -169,7 +169,7 @@ __global__ __launch_bounds__(VPT == 1 ? 1024 : 512) void norm_backward_kernel(No
     col.weight(w2, p.w_pre, p.H);
     float dw1[VPT][8] = {}, dw2[VPT][8] = {};
     // The next row is asked for before this one is worked on, into other registers: one workgroup a compute unit keeps the
-    // memory busy, and few rows are open at a time.  (Four groups a lane leave no registers for that.)
+    // memory busy, and few rows are open at a time.  (Two groups a lane leave no registers for that.)
     constexpr bool AHEAD = VPT == 1;
     struct Row {
         Raw8<F32> r[VPT], up[VPT];
@@ -372,10 +372,10 @@ static NormShape forward_shape(int64_t H) { return shape_of(H, H <= 512 ? 1 : H 
 static int64_t forward_grid(int64_t N, int64_t H, int R) { return std::min<int64_t>((N + R - 1) / R, H <= 512 ? 8192 : 1 << 22); }
 // Backward: a group a lane, so that the wavefronts of a row spread over the four SIMDs (5120 columns: 10 wavefronts; with two
 // groups 5, of which one SIMD has two: 32768 x 5120 with a gate for each element 620 us against 493) and 1024 threads have
-// the registers for two rows.  Above 8192 columns four groups, and a row at a time.  Rows of one wavefront, which wait for no other, come by 16
-// (262144 x 256: 184 us, 215 by 8).
+// the registers for two rows.  Above 8192 columns two groups, and a row at a time (14731 x 10176 with a row gate: 384 us, 412 with four
+// groups in half the wavefronts).  Rows of one wavefront, which wait for no other, come by 16 (262144 x 256: 184 us, 215 by 8).
 static NormShape backward_shape(int64_t H) {
-    return H <= 512 ? shape_of(H, 1, 16) : shape_of(H, H <= 8192 ? 1 : 4, 8);
+    return H <= 512 ? shape_of(H, 1, 16) : shape_of(H, H <= 8192 ? 1 : 2, 8);
 }
 static int64_t norm_parts(int64_t N, int64_t H) {
     const NormShape s = backward_shape(H);
@@ -460,10 +460,10 @@ int alst_block_norm_backward(const void* residual_out, const void* branch, const
     const NormShape s = backward_shape(H);
     const bool f32 = flags & ALST_FLAG_RESIDUAL_FP32;
     using Kernel = void (*)(NormParams);
-    static const Kernel kernels[2][2][2] = {{{norm_backward_kernel<false, false, 1>, norm_backward_kernel<false, false, 4>},
-                                             {norm_backward_kernel<false, true, 1>, norm_backward_kernel<false, true, 4>}},
-                                            {{norm_backward_kernel<true, false, 1>, norm_backward_kernel<true, false, 4>},
-                                             {norm_backward_kernel<true, true, 1>, norm_backward_kernel<true, true, 4>}}};
+    static const Kernel kernels[2][2][2] = {{{norm_backward_kernel<false, false, 1>, norm_backward_kernel<false, false, 2>},
+                                             {norm_backward_kernel<false, true, 1>, norm_backward_kernel<false, true, 2>}},
+                                            {{norm_backward_kernel<true, false, 1>, norm_backward_kernel<true, false, 2>},
+                                             {norm_backward_kernel<true, true, 1>, norm_backward_kernel<true, true, 2>}}};
     const Kernel kernel = kernels[f32][gate_cols > 1][s.vpt > 1];
     const int grid = (int)norm_parts(N, H);
     const size_t lds = std::max<size_t>(kPlaces * s.R * sizeof(float4), s.R > 1 ? s.R * H * sizeof(float) : 0);
