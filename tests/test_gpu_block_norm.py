@@ -12,7 +12,7 @@ from tests import step_util as U
 pytestmark = pytest.mark.gpu
 
 # fp32 operations on the longest path of an output: products and sums of one element (at most 12 each way), a row's sum of H
-# squares (8 to 16 a lane, 6 across lanes, up to 16 wavefronts) halved by the square root; backward goes through two norms.
+# squares (8 to 32 a lane, 6 across lanes, up to 16 wavefronts) halved by the square root; backward goes through two norms.
 FORWARD, BACKWARD = 64, 160
 # of a weight's gradient besides: the rows of a workgroup (here at most 9) of up to 16 at a time, up to 4 partial sums a thread, 4 and
 # 16 of these
