@@ -2,8 +2,8 @@
 //
 // A row is held in the registers of W wavefronts, 8 * VPT values a lane, so that everything is read and written once; its
 // sums (mean squares, and in backward the two products of a norm's gradient) go over the wavefronts through LDS.  Both are
-// bound by HBM: forward at 32768 x 4096 (norms before and after, 1.07 GB) 184 us = 5.8 TB/s, backward at 256000 x 4096 (12.6 GB)
-// 2.34 ms = 5.4 TB/s, of the 5.5 to 5.7 that a kernel reaches here that only reads four matrices and writes two.
+// bound by HBM: forward at 32768 x 4096 (norms before and after, 1.07 GB) 180 us = 6.0 TB/s, backward at 256000 x 4096 (12.6 GB)
+// 2.34 to 2.38 ms = 5.3 TB/s, of the 5.5 to 5.7 that a kernel reaches here that only reads four matrices and writes two.
 // Values stay packed bf16 in the registers between the passes over a row (stay_packed, made_here): with the conversions and
 // sums where the compiler puts them backward needs twice the registers and took 5.3 ms.
 #include <algorithm>
@@ -91,7 +91,7 @@ struct Columns {
 };
 
 // DENSE: a gate for each element.  Absent matrices read as zeros, absent weights as ones: the arithmetic has no branches.
-template <bool F32, bool DENSE, int VPT>
+template <bool F32, bool DENSE, int VPT, bool STREAMS>
 __global__ __launch_bounds__(512) void norm_forward_kernel(NormParams p) {
     extern __shared__ float lds[];
     RowPlace at(lds);
@@ -140,7 +140,7 @@ __global__ __launch_bounds__(512) void norm_forward_kernel(NormParams p) {
                 x[v][k] = r[v].get(k) + change;
                 xx[0] = fmaf(x[v][k], x[v][k], xx[0]);
             }
-            residual_out.store(col.at[v], x[v]);
+            residual_out.template store<STREAMS>(col.at[v], x[v]);
         }
         if (pre) {
             at.sum(xx);
@@ -150,13 +150,13 @@ __global__ __launch_bounds__(512) void norm_forward_kernel(NormParams p) {
                 float n[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) n[k] = x[v][k] * q2 * (w2[v].get(k) + p.offset);
-                normed.store(col.at[v], n);
+                normed.template store<STREAMS>(col.at[v], n);
             }
         }
     }
 }
 
-template <bool F32, bool DENSE, int VPT>
+template <bool F32, bool DENSE, int VPT, bool STREAMS>
 __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
     extern __shared__ float lds[];
     RowPlace at(lds);
@@ -234,7 +234,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
                 dw2[v][k] = fmaf(d, x * q2, dw2[v][k]);
             }
             made_here(dw2[v]);
-            d_residual.store(col.at[v], g[v]);
+            d_residual.template store<STREAMS>(col.at[v], g[v]);
         }
         // dp, in g's place, and the sum over the row of dp (w_post + o) b: the norm's gradient and a row's gate both take it
         const Gate row_gate = row_gated ? gate_of(__uint_as_float((uint32_t)row.gate << 16)) : Gate{1.f, 0.f};
@@ -272,8 +272,8 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
                 if (DENSE) dz[k] = g[v][k] * gate_of(z[v].get(k)).off * (q1 * w * y);
                 o[k] = q1 * fmaf(g[v][k], w, -y * c1);
             }
-            d_branch.store(col.at[v], o);
-            if (DENSE) d_gate.store(col.at[v], dz);
+            d_branch.template store<STREAMS>(col.at[v], o);
+            if (DENSE) d_gate.template store<STREAMS>(col.at[v], dz);
         }
     };
     const int64_t step = (int64_t)gridDim.x * at.R, first = (int64_t)blockIdx.x * at.R;
@@ -377,6 +377,25 @@ static int64_t forward_grid(int64_t N, int64_t H, int R) { return std::min<int64
 static NormShape backward_shape(int64_t H) {
     return H <= 512 ? shape_of(H, 1, 16) : shape_of(H, H <= 8192 ? 1 : 2, 8);
 }
+using NormKernel = void (*)(NormParams);
+template <bool S>
+static NormKernel forward_kernel(bool f32, bool dense, int vpt) {
+    static const NormKernel kernels[2][2][3] = {
+        {{norm_forward_kernel<false, false, 1, S>, norm_forward_kernel<false, false, 2, S>, norm_forward_kernel<false, false, 4, S>},
+         {norm_forward_kernel<false, true, 1, S>, norm_forward_kernel<false, true, 2, S>, norm_forward_kernel<false, true, 4, S>}},
+        {{norm_forward_kernel<true, false, 1, S>, norm_forward_kernel<true, false, 2, S>, norm_forward_kernel<true, false, 4, S>},
+         {norm_forward_kernel<true, true, 1, S>, norm_forward_kernel<true, true, 2, S>, norm_forward_kernel<true, true, 4, S>}}};
+    return kernels[f32][dense][vpt >> 1];
+}
+template <bool S>
+static NormKernel backward_kernel(bool f32, bool dense, int vpt) {
+    static const NormKernel kernels[2][2][2] = {
+        {{norm_backward_kernel<false, false, 1, S>, norm_backward_kernel<false, false, 2, S>},
+         {norm_backward_kernel<false, true, 1, S>, norm_backward_kernel<false, true, 2, S>}},
+        {{norm_backward_kernel<true, false, 1, S>, norm_backward_kernel<true, false, 2, S>},
+         {norm_backward_kernel<true, true, 1, S>, norm_backward_kernel<true, true, 2, S>}}};
+    return kernels[f32][dense][vpt > 1];
+}
 static int64_t norm_parts(int64_t N, int64_t H) {
     const NormShape s = backward_shape(H);
     return std::min<int64_t>((N + s.R - 1) / s.R, kMaxNormParts);
@@ -424,13 +443,8 @@ int alst_block_norm_forward(const void* residual, const void* branch, const void
     p.H = (int)H; p.gate_cols = (int)gate_cols;
     const NormShape s = forward_shape(H);
     const bool f32 = flags & ALST_FLAG_RESIDUAL_FP32;
-    using Kernel = void (*)(NormParams);
-    static const Kernel kernels[2][2][3] = {
-        {{norm_forward_kernel<false, false, 1>, norm_forward_kernel<false, false, 2>, norm_forward_kernel<false, false, 4>},
-         {norm_forward_kernel<false, true, 1>, norm_forward_kernel<false, true, 2>, norm_forward_kernel<false, true, 4>}},
-        {{norm_forward_kernel<true, false, 1>, norm_forward_kernel<true, false, 2>, norm_forward_kernel<true, false, 4>},
-         {norm_forward_kernel<true, true, 1>, norm_forward_kernel<true, true, 2>, norm_forward_kernel<true, true, 4>}}};
-    const Kernel kernel = kernels[f32][gate_cols > 1][s.vpt >> 1];
+    const NormKernel kernel = streams_out(N * H * 2) ? forward_kernel<true>(f32, gate_cols > 1, s.vpt)
+                                                     : forward_kernel<false>(f32, gate_cols > 1, s.vpt);
     const int64_t grid = forward_grid(N, H, s.R);
     hipLaunchKernelGGL(kernel, dim3((unsigned)grid), dim3(s.W * 64, s.R), kPlaces * s.R * sizeof(float4), (hipStream_t)stream, p);
     return hipGetLastError() == hipSuccess ? ALST_OK : ALST_ERR_HIP;
@@ -459,12 +473,8 @@ int alst_block_norm_backward(const void* residual_out, const void* branch, const
     p.H = (int)H; p.gate_cols = (int)gate_cols;
     const NormShape s = backward_shape(H);
     const bool f32 = flags & ALST_FLAG_RESIDUAL_FP32;
-    using Kernel = void (*)(NormParams);
-    static const Kernel kernels[2][2][2] = {{{norm_backward_kernel<false, false, 1>, norm_backward_kernel<false, false, 2>},
-                                             {norm_backward_kernel<false, true, 1>, norm_backward_kernel<false, true, 2>}},
-                                            {{norm_backward_kernel<true, false, 1>, norm_backward_kernel<true, false, 2>},
-                                             {norm_backward_kernel<true, true, 1>, norm_backward_kernel<true, true, 2>}}};
-    const Kernel kernel = kernels[f32][gate_cols > 1][s.vpt > 1];
+    const NormKernel kernel = streams_out(N * H * 2) ? backward_kernel<true>(f32, gate_cols > 1, s.vpt)
+                                                     : backward_kernel<false>(f32, gate_cols > 1, s.vpt);
     const int grid = (int)norm_parts(N, H);
     const size_t lds = std::max<size_t>(kPlaces * s.R * sizeof(float4), s.R > 1 ? s.R * H * sizeof(float) : 0);
     hipLaunchKernelGGL(kernel, dim3(grid), dim3(s.W * 64, s.R), lds, (hipStream_t)stream, p);

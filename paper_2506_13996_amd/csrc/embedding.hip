@@ -6,9 +6,10 @@
 // writes it out when the token changes.  Only a token of more rows than a range is cut; join_kernel adds up its partial sums.
 // Rows of tokens that do not occur are filled with zeros beside the steps that leave the memory idle.
 //
-// Both are bound by HBM.  131072 rows of 4096 by Zipf-distributed tokens: lookup 245 us = 5.1 TB/s.  Their gradient over 128256 tokens
-// 459 us = 4.6 TB/s: 36 us of sort, 300 us of sums (1.07 GB of rows in the tokens' order, which come at 4.5 TB/s; rows in the order
-// of memory at 5.5), the rest zeros (at 6 TB/s).
+// Both are bound by HBM.  131072 rows of 4096 by Zipf-distributed tokens: lookup 217 us = 5.8 TB/s (245 with results written through the
+// caches).  Their gradient over 128256 tokens 433 us = 4.9 TB/s (457): 36 us of sort, about 280 of sums (1.07 GB of rows in the
+// tokens' order, which come at 4.5 TB/s; rows in the order of memory at 5.5), the rest zeros.  The pairs of figures below that chose
+// between two forms were measured before results were written past the caches.
 #include <algorithm>
 
 #include "../../include/alst_embedding.h"
@@ -24,7 +25,7 @@ constexpr int64_t kMostGroups = 1 << 22;        // workgroups of a launch (their
 constexpr int kForwardColumns = 1024;          // of a wavefront: two groups of eight values a lane
 // W wavefronts (blockDim.x / 64) take ROWS rows, 1024 columns each; the R rows of wavefronts of a workgroup lie behind each other.
 // A token that takes no part has no row: it is read as zeros.
-template <bool F32, int ROWS>
+template <bool F32, int ROWS, bool STREAMS>
 __global__ __launch_bounds__(256) void embedding_forward_kernel(const int32_t* __restrict__ tokens, const uint16_t* __restrict__ E,
                                                                 void* __restrict__ y, int64_t N, int H, int V, int ignore_index,
                                                                 float scale, int32_t* __restrict__ status) {
@@ -54,7 +55,7 @@ __global__ __launch_bounds__(256) void embedding_forward_kernel(const int32_t* _
                 float v[8];
 #pragma unroll
                 for (int k = 0; k < 8; ++k) v[k] = r[j][c].get(k) * factor[j];
-                row.store(col + c * next, v);
+                row.template store<STREAMS>(col + c * next, v);
             }
         }
     }
@@ -101,7 +102,13 @@ struct ZeroRows {
     const uint8_t* occurs;       // [V]; NULL: every row
     int64_t from, upto;
     int halves;                  // of a row: its bytes / 2
+    bool streams;
     __device__ __forceinline__ void run(int64_t group, int64_t groups) const {
+        if (streams) run_as<true>(group, groups);
+        else run_as<false>(group, groups);
+    }
+    template <bool STREAMS>
+    __device__ __forceinline__ void run_as(int64_t group, int64_t groups) const {
         const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
         const int slabs = (halves + 511) / 512, rows = max(1, waves / slabs), mine = wave / slabs, slab = wave - mine * slabs;
         if (mine >= rows) return;
@@ -112,7 +119,7 @@ struct ZeroRows {
             for (int v = mine; v < kZeroRows; v += rows) {
                 if (!(absent >> v & 1)) continue;
                 const RowBuffer<false> row(dE, v0 + v, halves, true);
-                for (int c = slab; c < slabs; c += step) row.store(c * 512 + lane * 8, zeros);
+                for (int c = slab; c < slabs; c += step) row.template store<STREAMS>(c * 512 + lane * 8, zeros);
             }
         }
     }
@@ -281,7 +288,7 @@ struct Grad {
     bool f32, accumulate;
 };
 
-template <bool F32>
+template <bool F32, bool STREAMS>
 __device__ __forceinline__ void write_grad_as(const Grad& g, int key, int H, uint32_t col, const float (&sum)[8]) {
     const RowBuffer<F32> row(g.dE, key, H, true);
     float v[8];
@@ -292,11 +299,12 @@ __device__ __forceinline__ void write_grad_as(const Grad& g, int key, int H, uin
 #pragma unroll
         for (int k = 0; k < 8; ++k) v[k] += old.get(k);
     }
-    row.store(col, v);
+    row.template store<STREAMS>(col, v);
 }
+template <bool STREAMS>
 __device__ __forceinline__ void write_grad(const Grad& g, int key, int H, uint32_t col, const float (&sum)[8]) {
-    if (g.f32) write_grad_as<true>(g, key, H, col, sum);
-    else write_grad_as<false>(g, key, H, col, sum);
+    if (g.f32) write_grad_as<true, false>(g, key, H, col, sum);
+    else write_grad_as<false, STREAMS>(g, key, H, col, sum);
 }
 
 constexpr int kSumThreads = 512;
@@ -308,7 +316,7 @@ constexpr int kJoinGroups = 256;               // workgroups of the joins' launc
 // Only a token that goes through a whole range besides is cut: parts[range][1] has its rows of the range where it begins, which is
 // then listed, parts[range][0] those of the ranges behind.  A workgroup: a range and 512 columns a wavefront; workgroups from
 // `ranges` on: rows of zeros.
-template <bool F32>
+template <bool F32, bool STREAMS>
 __global__ __launch_bounds__(kSumThreads) void run_sums_kernel(const Pair* __restrict__ pairs, const void* __restrict__ dy, int64_t N,
                                                                int H, int V, int run, int64_t ranges, float* __restrict__ parts,
                                                                Pair* __restrict__ list, EmbeddingHeader* header, Grad g, ZeroRows zeros) {
@@ -364,7 +372,7 @@ __global__ __launch_bounds__(kSumThreads) void run_sums_kernel(const Pair* __res
                     RowBuffer<true>(parts, range * 2 + 1, H, true).store(col, sum);
                     if (blockIdx.y == 0 && threadIdx.x == 0) list[atomicAdd(&header->joins, 1)] = {key, (int32_t)range};
                 } else {
-                    write_grad(g, key, H, col, sum);
+                    write_grad<STREAMS>(g, key, H, col, sum);
                 }
                 head = false;
 #pragma unroll
@@ -428,7 +436,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Pair* __restri
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum[j] += r.get(j);
             }
-            write_grad(g, key, H, col, sum);
+            write_grad<false>(g, key, H, col, sum);
         }
         __syncthreads();
     }
@@ -518,8 +526,13 @@ int alst_embedding_forward(const int32_t* tokens, const void* E, int64_t N, int6
     const int64_t rows = (int64_t)R * together, columns = (int64_t)W * kForwardColumns;
     const dim3 grid((unsigned)std::min((N + rows - 1) / rows, kMostGroups), (unsigned)((H + columns - 1) / columns));
     const bool f32 = flags & ALST_FLAG_RESIDUAL_FP32;
-    auto kernel = together == 1 ? (f32 ? embedding_forward_kernel<true, 1> : embedding_forward_kernel<false, 1>)
-                                : (f32 ? embedding_forward_kernel<true, 4> : embedding_forward_kernel<false, 4>);
+    const bool streams = streams_out(N * H * 2);
+    auto kernel = together == 1 ? (f32       ? embedding_forward_kernel<true, 1, false>
+                                   : streams ? embedding_forward_kernel<false, 1, true>
+                                             : embedding_forward_kernel<false, 1, false>)
+                                : (f32       ? embedding_forward_kernel<true, 4, false>
+                                   : streams ? embedding_forward_kernel<false, 4, true>
+                                             : embedding_forward_kernel<false, 4, false>);
     hipLaunchKernelGGL(kernel, grid, dim3(W * 64, R), 0, (hipStream_t)stream, tokens, (const uint16_t*)E, y, N, (int)H, (int)V,
                        ignore_index, scale, device_status_out);
     return hipGetLastError() == hipSuccess ? ALST_OK : ALST_ERR_HIP;
@@ -538,12 +551,14 @@ int alst_embedding_backward(const int32_t* tokens, const void* dy, int64_t N, in
     unsigned char* const ws = static_cast<unsigned char*>(workspace);
     EmbeddingHeader* const header = reinterpret_cast<EmbeddingHeader*>(ws);
     float* const parts = reinterpret_cast<float*>(ws + L.parts);
-    const Grad g = {dE, scale, (flags & ALST_FLAG_DW_FP32) != 0, (flags & ALST_FLAG_DW_ACCUMULATE) != 0};
+    const bool sums32 = flags & ALST_FLAG_DW_FP32;
+    const int64_t row_bytes = H * (sums32 ? 4 : 2);
+    const Grad g = {dE, scale, sums32, (flags & ALST_FLAG_DW_ACCUMULATE) != 0};
+    const bool streams = streams_out(V * row_bytes);
     uint8_t* const occurs = g.accumulate ? nullptr : ws + L.occurs;
     // rows of zeros: a share beside each step of the sort (whose few workgroups leave the memory idle for about that many bytes'
     // time), the rest beside the sums
-    const int64_t row_bytes = H * (g.f32 ? 4 : 2);
-    ZeroRows zeros = {dE, occurs, 0, 0, (int)(row_bytes / 2)};
+    ZeroRows zeros = {dE, occurs, 0, 0, (int)(row_bytes / 2), streams};
     auto take_zeros = [&](int64_t bytes) {               // workgroups of 16 wavefronts that fill the next `bytes`
         zeros.from = zeros.upto;
         if (g.accumulate || bytes == 0) return 0;
@@ -583,7 +598,8 @@ int alst_embedding_backward(const int32_t* tokens, const void* dy, int64_t N, in
     take_zeros(join ? std::max<int64_t>(left - kZerosBesideJoins, 0) : left);
     const int64_t fill = std::min((zeros.groups() + columns - 1) / columns, kMostGroups);
     Pair* const list = reinterpret_cast<Pair*>(ws + L.list);
-    auto sums = flags & ALST_FLAG_RESIDUAL_FP32 ? run_sums_kernel<true> : run_sums_kernel<false>;
+    auto sums = flags & ALST_FLAG_RESIDUAL_FP32 ? (streams ? run_sums_kernel<true, true> : run_sums_kernel<true, false>)
+                                                : (streams ? run_sums_kernel<false, true> : run_sums_kernel<false, false>);
     hipLaunchKernelGGL(sums, dim3((unsigned)(L.ranges + fill), (unsigned)columns), dim3(waves * 64), 0, s, src.pairs, dy, N, (int)H, (int)V,
                        L.run, L.ranges, parts, list, header, g, zeros);
     if (join) {

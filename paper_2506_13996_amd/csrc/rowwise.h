@@ -98,7 +98,9 @@ struct RowBuffer {
         }
         return r;
     }
-    __device__ __forceinline__ void store(uint32_t at, const float (&v)[8]) const {      // rounded once
+    // Rounded once.  STREAMS: of a matrix that no cache will hold (bf16 only: fp32 values of a lane fill half a line an instruction).
+    template <bool STREAMS = false>
+    __device__ __forceinline__ void store(uint32_t at, const float (&v)[8]) const {
         if constexpr (F32) {
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, make_float4(v[0], v[1], v[2], v[3])), rsrc, at * 4, 0, 0);
             __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, make_float4(v[4], v[5], v[6], v[7])), rsrc, at * 4 + 16, 0, 0);
@@ -106,7 +108,7 @@ struct RowBuffer {
             bf16x8_t o;
 #pragma unroll
             for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), rsrc, at * 2, 0, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4_t, o), rsrc, at * 2, 0, STREAMS ? 2 : 0);      // (2: non-temporal)
         }
     }
 };
@@ -133,6 +135,11 @@ __device__ __forceinline__ double wave_sum(double v) {
     for (int step = 1; step < 64; step <<= 1) v += __shfl_xor(v, step);
     return v;
 }
+
+// Whether a result of so many bytes is written past the caches.  Behind them is a memory-side cache of 256 MB, from which the next
+// call reads a short result: lookup and the norm that reads its rows, both results written so, 8192 x 4096 (64 MB each) 42.7 -> 45.0
+// us, 16384 x 4096 89 -> 84, 32768 x 4096 194 -> 173.
+static inline bool streams_out(int64_t bytes) { return bytes >= (int64_t)96 << 20; }
 
 static inline bool aligned_to(const void* p, uintptr_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
 
