@@ -150,6 +150,7 @@ __device__ __forceinline__ uint4 scaled(uint4 q, float c, bool f32) {
 
 // out = g * c.  Every workgroup adds the partial sums up by itself (n = 1: the sum is there), which pays while there are few
 // workgroups: one launch fewer.  The first one writes them down.
+template <bool STREAMS>
 __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradList L, const double* __restrict__ parts, int n, float max_norm,
                                                              double* __restrict__ sumsq_out, float* __restrict__ norm_out) {
     __shared__ double lds[kThreads / 64];
@@ -181,7 +182,12 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradList L, const d
 #pragma unroll
             for (int j = 0; j < kLinesEach; ++j) q[j] = p[j * kThreads];
 #pragma unroll
-            for (int j = 0; j < kLinesEach; ++j) o[j * kThreads] = clip ? scaled(q[j], c, f32) : q[j];
+            for (int j = 0; j < kLinesEach; ++j) {
+                const u32x4_t w = __builtin_bit_cast(u32x4_t, clip ? scaled(q[j], c, f32) : q[j]);
+                u32x4_t* const at = reinterpret_cast<u32x4_t*>(o + j * kThreads);
+                if (STREAMS) __builtin_nontemporal_store(w, at);
+                else *at = w;
+            }
             continue;
         }
         // a chunk at a tensor's end, or of an output at another 16-byte phase: by elements, neighbours in neighbouring lanes
@@ -259,11 +265,15 @@ static int run_squares(const alst_grad_tensor* ts, int64_t count, double* parts,
 
 static int run_clip(const alst_grad_tensor* ts, int64_t count, const double* parts, int n, float max_norm, double* sumsq_out,
                     float* norm_out, hipStream_t s) {
+    int64_t bytes = 0;
+    for (int64_t i = 0; i < count; ++i) bytes += ts[i].n * (ts[i].fp32 ? 4 : 2);
+    // (the gradients are read a second time, so what is written besides should not take their place in the caches: 355 MB 202 -> 188 us)
+    auto kernel = streams_out(bytes) ? grad_clip_kernel<true> : grad_clip_kernel<false>;
     bool first = true;
     for (int64_t at = 0; at < count || first;) {
         const GradList L = take_listed(ts, count, at);
         // (a list of empty tensors still has a norm)
-        hipLaunchKernelGGL(grad_clip_kernel, dim3(std::max<uint32_t>(std::min(L.first[L.count], kMostClipGroups), 1)), dim3(kThreads), 0, s, L, parts, n, max_norm,
+        hipLaunchKernelGGL(kernel, dim3(std::max<uint32_t>(std::min(L.first[L.count], kMostClipGroups), 1)), dim3(kThreads), 0, s, L, parts, n, max_norm,
                            first ? sumsq_out : nullptr, first ? norm_out : nullptr);
         first = false;
     }

@@ -83,3 +83,22 @@ def test_block_norms(H, fp32, gate):
     for k, t in enumerate(dw):          # other orders of the rows' sum: half a step of fp32 at the sum of magnitudes for each row of a workgroup
         both = halves[0][1][k].double() + halves[1][1][k].double()
         assert (t.double() - both).abs().max() <= (N / 256 + 200) * U.FP32 * 40 * N ** 0.5 * both.abs().max().clamp(min=1)
+
+
+def test_clipping():
+    n = LIMIT // 2 + 12345
+    g = torch.Generator(device="cuda").manual_seed(1)
+    grads = [torch.randn(n, generator=g, device="cuda").to(torch.bfloat16), torch.randn(777, generator=g, device="cuda")]
+    sumsq = torch.full((1,), 4.0 * n, dtype=torch.float64, device="cuda")
+    outs = [U.Guarded((n,), torch.bfloat16), U.Guarded((777,), torch.float32)]
+    B.alst_grad_clip(B.GradTensors(grads, [o.t for o in outs]), sumsq, 100.0)
+    parts = [torch.empty_like(t) for t in grads]
+    for s in _halves(n):
+        B.alst_grad_clip(B.GradTensors([grads[0][s]], [parts[0][s]]), sumsq, 100.0)
+    B.alst_grad_clip(B.GradTensors(grads[1:], parts[1:]), sumsq, 100.0)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o.t, p) and o.intact() for o, p in zip(outs, parts))
+    want = grads[0].double() * (100.0 / (4.0 * n) ** 0.5)
+    assert ((outs[0].t.double() - want).abs() <= want.abs() * (U.half_step(torch.bfloat16) + 2 * U.FP32)).all()
+    B.alst_grad_clip(grads, sumsq, 100.0)          # in place
+    assert all(torch.equal(a, b) for a, b in zip(grads, parts))
