@@ -60,7 +60,8 @@ int alst_block_norm_forward(const void* residual, const void* branch, const void
                             void* stream);
 
 /*
- *   residual_out    [N,H] r' as forward wrote it (without a branch: forward's `residual`)
+ *   residual_out    [N,H] r' as forward wrote it (without a branch: forward's `residual`); without w_pre it is not
+ *                   read and may be NULL
  *   d_normed        [N,H] dn; NULL exactly if w_pre is
  *   d_residual_out  [N,H] dr', or NULL for zeros (only with w_pre)
  *   d_residual      [N,H] dr, overwritten; may be `d_residual_out` itself; NULL only if there is no w_pre: dr is
@@ -70,8 +71,8 @@ int alst_block_norm_forward(const void* residual, const void* branch, const void
  *   dw_post, dw_pre [H] bf16 (fp32 with ALST_FLAG_DW_FP32); overwritten, or += with ALST_FLAG_DW_ACCUMULATE;
  *                   NULL exactly if the weight is.  Sums over the rows are fp32, in an order that depends on N
  *                   and H alone.
- *   branch          may be NULL if there is neither w_post nor a gate, in which case its value is not needed;
- *                   d_branch then says that there is a branch
+ *   branch          may be NULL if there is neither w_post nor a gate, and is not read then; d_branch says that there
+ *                   is a branch
  * Apart from that no output may overlap another buffer.
  */
 int alst_block_norm_backward(const void* residual_out, const void* branch, const void* w_post,
