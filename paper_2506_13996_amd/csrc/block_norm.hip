@@ -262,7 +262,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
             const __bf16 dz = (__bf16)(row_gate.off * q1 * vb[0]);
             p.d_gate[i] = __builtin_bit_cast(uint16_t, dz);
         }
-        const float c1 = post ? q1 * q1 * vb[0] * inv_h : 0.f;
+        const float c1 = q1 * q1 * vb[0] * inv_h;
 #pragma unroll
         for (int v = 0; v < VPT; ++v) {
             float o[8], dz[8];
@@ -270,7 +270,8 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
             for (int k = 0; k < 8; ++k) {
                 const float w = w1[v].get(k) + o1, y = b[v].get(k);
                 if (DENSE) dz[k] = g[v][k] * gate_of(z[v].get(k)).off * (q1 * w * y);
-                o[k] = q1 * fmaf(g[v][k], w, -y * c1);
+                const float rest = y * c1;     // (without a norm after the block left out: an infinity in b would come in as inf * 0)
+                o[k] = q1 * fmaf(g[v][k], w, post ? -rest : 0.f);
             }
             d_branch.template store<STREAMS>(col.at[v], o);
             if (DENSE) d_gate.template store<STREAMS>(col.at[v], dz);
