@@ -438,7 +438,9 @@ int alst_block_norm_forward(const void* residual, const void* branch, const void
     NormParams p = {};
     p.residual = residual; p.branch = (const uint16_t*)branch; p.w_post = (const uint16_t*)w_post; p.gate = (const uint16_t*)gate;
     p.w_pre = (const uint16_t*)w_pre; p.residual_out = residual_out; p.normed = (uint16_t*)normed;
-    p.N = N; p.scale = branch_scale; p.eps = eps; p.offset = weight_offset;
+    p.N = N; p.eps = eps;
+    p.scale = branch ? branch_scale : 0.f;                   // (absent parts are zeros and ones to the kernel,
+    p.offset = w_post || w_pre ? weight_offset : 0.f;        //  whose results go by no scale or offset)
     const int rc = validate_norm(p, H, gate_cols);
     if (rc != ALST_OK) return rc;
     p.H = (int)H; p.gate_cols = (int)gate_cols;
@@ -466,7 +468,8 @@ int alst_block_norm_backward(const void* residual_out, const void* branch, const
     p.residual = residual_out; p.branch = (const uint16_t*)branch; p.w_post = (const uint16_t*)w_post; p.gate = (const uint16_t*)gate;
     p.w_pre = (const uint16_t*)w_pre; p.d_normed = (const uint16_t*)d_normed; p.d_residual_out = d_residual_out;
     p.d_residual = d_residual; p.d_branch = (uint16_t*)d_branch; p.d_gate = (uint16_t*)d_gate; p.parts = (float*)workspace;
-    p.N = N; p.scale = branch_scale; p.eps = eps; p.offset = weight_offset;
+    p.N = N; p.scale = branch_scale; p.eps = eps;
+    p.offset = w_post || w_pre ? weight_offset : 0.f;
     int rc = validate_norm(p, H, gate_cols);
     if (rc == ALST_OK && !(aligned_to(dw_pre, 16) && aligned_to(dw_post, 16))) rc = ALST_ERR_ALIGN;
     if (rc == ALST_OK && (w_pre || w_post) && workspace_bytes < alst_block_norm_workspace_bytes(N, H)) rc = ALST_ERR_WORKSPACE;
