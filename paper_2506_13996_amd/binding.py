@@ -561,7 +561,8 @@ class GradTensors:
     (None: in place).  Keeps the tensors alive."""
 
     def __init__(self, grads, outs=None):
-        self.grads, self.outs = list(grads), list(grads if outs is None else outs)
+        self.grads = list(grads)      # (once: it may be an iterator)
+        self.outs = list(self.grads if outs is None else outs)
         if len(self.grads) != len(self.outs):
             raise TypeError(f"{len(self.grads)} gradients and {len(self.outs)} outs")
         self.array = (GradTensor * max(1, len(self.grads)))()
