@@ -131,17 +131,30 @@ __global__ __launch_bounds__(kThreads) void grad_norm_kernel(const double* __res
     }
 }
 
-__device__ __forceinline__ uint4 scaled(uint4 q, float c, bool f32) {
+// The factor min(1, max_norm / norm) as c * 2^e.  e is 0 unless the factor is below the normal numbers of fp32, where few or none of
+// its bits would be left; v * c stays finite, as |v| <= norm < 2^128 and so |v * c| <= norm * factor * 2^-e < 2^127.
+// e by two comparisons: 7 tensors of 3.3 MB 9.8 us, with frexp of the factor 10.9.
+struct Factor {
+    float c;
+    int e;
+    __device__ __forceinline__ float times(float v) const { return __builtin_ldexpf(v * c, e); }
+};
+__device__ __forceinline__ Factor factor_of(double ratio) {
+    const bool low = ratio < 0x1p-126, very = ratio < 0x1p-251;
+    return {(float)(ratio * (very ? 0x1p250 : low ? 0x1p125 : 1.0)), very ? -250 : low ? -125 : 0};
+}
+
+__device__ __forceinline__ uint4 scaled(uint4 q, const Factor& c, bool f32) {
     uint32_t* const w = &q.x;
     if (f32) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(__uint_as_float(w[i]) * c);
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(c.times(__uint_as_float(w[i])));
     } else {
         bf16x8_t o;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            o[2 * i] = (__bf16)(__uint_as_float(w[i] << 16) * c);
-            o[2 * i + 1] = (__bf16)(__uint_as_float(w[i] & 0xffff0000u) * c);
+            o[2 * i] = (__bf16)c.times(__uint_as_float(w[i] << 16));
+            o[2 * i + 1] = (__bf16)c.times(__uint_as_float(w[i] & 0xffff0000u));
         }
         q = __builtin_bit_cast(uint4, o);
     }
@@ -161,7 +174,7 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradList L, const d
     }
     // (a norm that is not finite, in fp32 as it is reported, scales nothing)
     const bool clip = norm > (double)max_norm && isfinite((float)norm);
-    const float c = clip ? (float)((double)max_norm / norm) : 1.f;
+    const Factor c = factor_of(clip ? (double)max_norm / norm : 1.0);
     const uint32_t chunks = L.first[L.count];
     for (uint32_t k = blockIdx.x; k < chunks; k += gridDim.x) {
         const int t = tensor_of(L, k);
@@ -195,10 +208,10 @@ __global__ __launch_bounds__(kThreads) void grad_clip_kernel(GradList L, const d
         for (int64_t e = from + (int64_t)threadIdx.x * size; e < upto; e += kThreads * size) {
             if (f32) {
                 const float v = *reinterpret_cast<const float*>(line0 + e);
-                *reinterpret_cast<float*>(out0 + e) = clip ? v * c : v;
+                *reinterpret_cast<float*>(out0 + e) = clip ? c.times(v) : v;
             } else {
                 const uint16_t v = *reinterpret_cast<const uint16_t*>(line0 + e);
-                const __bf16 o = (__bf16)(__uint_as_float((uint32_t)v << 16) * c);
+                const __bf16 o = (__bf16)c.times(__uint_as_float((uint32_t)v << 16));
                 *reinterpret_cast<uint16_t*>(out0 + e) = clip ? __builtin_bit_cast(uint16_t, o) : v;
             }
         }
