@@ -26,7 +26,7 @@ extern "C" {
 
 /* Bytes of device scratch that alst_embedding_backward needs, 0 if the shape is invalid.  Pure host
  * arithmetic.  Large terms: 16 N bytes for the tokens in sorted order, V bytes for the tokens that occur, and fp32 sums of tokens
- * whose sorted rows are cut into ranges: N H / 8 bytes, in short calls up to N H and 32 MB.  A workspace serves every N up
+ * whose sorted rows are cut into ranges: N H / 16 bytes, in short calls up to N H and 32 MB.  A workspace serves every N up
  * to its own. */
 size_t alst_embedding_workspace_bytes(int64_t N, int64_t H, int64_t V);
 
