@@ -304,7 +304,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
             __syncthreads();
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
-                if (col.at[v] < (uint32_t)p.H) store8<true>(lds + at.row * p.H, col.at[v], which ? dw1[v] : dw2[v]);
+                if (col.at[v] < (uint32_t)p.H) store8(lds + at.row * p.H, col.at[v], which ? dw1[v] : dw2[v]);
             __syncthreads();
             for (int c = at.row * blockDim.x + at.tid; c < p.H; c += blockDim.x * at.R) {
                 float t = 0.f;
@@ -314,7 +314,7 @@ __global__ __launch_bounds__(1024) void norm_backward_kernel(NormParams p) {
         } else {
 #pragma unroll
             for (int v = 0; v < VPT; ++v)
-                if (col.at[v] < (uint32_t)p.H) store8<true>(part + which * p.H, col.at[v], which ? dw1[v] : dw2[v]);
+                if (col.at[v] < (uint32_t)p.H) store8(part + which * p.H, col.at[v], which ? dw1[v] : dw2[v]);
         }
     }
 }

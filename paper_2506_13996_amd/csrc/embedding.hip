@@ -427,12 +427,12 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Pair* __restri
             }
         };
         add(wave, kWaves);
-        if (wave != 0) store8<true>(lds[wave], lane * 8, sum);
+        if (wave != 0) store8(lds[wave], lane * 8, sum);
         __syncthreads();
         if (wave == 0) {
 #pragma unroll
             for (int w = 1; w < kWaves; ++w) {
-                const Raw8<true> r = load8<true>(lds[w], lane * 8);
+                const Raw8<true> r = load8(lds[w], lane * 8);
 #pragma unroll
                 for (int j = 0; j < 8; ++j) sum[j] += r.get(j);
             }

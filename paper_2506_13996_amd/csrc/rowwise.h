@@ -5,9 +5,9 @@
 #include <math.h>
 #include <stdint.h>
 
-#include "common.h"
-
 namespace alst {
+
+typedef __bf16 bf16x8_t __attribute__((ext_vector_type(8)));
 
 // Eight values of a row: 16 bytes of bf16, or 32 of fp32, as they were loaded (bf16 stays packed until it is used).
 template <bool F32> struct Raw8;
@@ -23,31 +23,15 @@ template <> struct Raw8<true> {
     __device__ __forceinline__ float get(int i) const { return (&q[i >> 2].x)[i & 3]; }
 };
 
-// A row of a matrix: a base that is the same for a wavefront, so that its elements are addressed by a scalar base and a 32-bit
-// offset of the lane.
-template <bool F32> __device__ __forceinline__ const char* row_of(const void* p, int64_t at) {
-    return static_cast<const char*>(p) + at * (F32 ? 4 : 2);
+// Eight fp32 values from element `at` of a row, a multiple of 4; the lane's offset stays in 32 bits.
+__device__ __forceinline__ Raw8<true> load8(const void* row, uint32_t at) {
+    const float4* const from = reinterpret_cast<const float4*>(static_cast<const char*>(row) + (size_t)(at * 4u));
+    return {{from[0], from[1]}};
 }
-template <bool F32> __device__ __forceinline__ char* row_of(void* p, int64_t at) { return static_cast<char*>(p) + at * (F32 ? 4 : 2); }
-
-template <bool F32>
-__device__ __forceinline__ Raw8<F32> load8(const void* row, uint32_t at) {      // element `at` of the row, a multiple of 8
-    Raw8<F32> r;
-    const char* const from = static_cast<const char*>(row) + (size_t)(at * (F32 ? 4u : 2u));
-    if constexpr (F32) {
-        r.q[0] = reinterpret_cast<const float4*>(from)[0];
-        r.q[1] = reinterpret_cast<const float4*>(from)[1];
-    } else {
-        r.q = *reinterpret_cast<const uint4*>(from);
-    }
-    return r;
-}
-template <bool F32>
-__device__ __forceinline__ Raw8<F32> zero8() {
-    Raw8<F32> r;
-    if constexpr (F32) r.q[0] = r.q[1] = make_float4(0.f, 0.f, 0.f, 0.f);
-    else r.q = make_uint4(0u, 0u, 0u, 0u);
-    return r;
+__device__ __forceinline__ void store8(void* row, uint32_t at, const float (&v)[8]) {
+    float4* const to = reinterpret_cast<float4*>(static_cast<char*>(row) + (size_t)(at * 4u));
+    to[0] = make_float4(v[0], v[1], v[2], v[3]);
+    to[1] = make_float4(v[4], v[5], v[6], v[7]);
 }
 
 // Keeps packed values packed through a loop: the compiler would convert them before it, twice the registers.
@@ -57,22 +41,6 @@ __device__ __forceinline__ void stay_packed(Raw8<true>&) {}
 // Has the values made here: the compiler would put sums off to the loop's end and keep their terms until then.
 __device__ __forceinline__ void made_here(float (&v)[8]) {
     asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));
-}
-
-// Eight fp32 values rounded once to the row's type.
-template <bool F32>
-__device__ __forceinline__ void store8(void* row, uint32_t at, const float (&v)[8]) {
-    char* const to = static_cast<char*>(row) + (size_t)(at * (F32 ? 4u : 2u));
-    if constexpr (F32) {
-        float4* f = reinterpret_cast<float4*>(to);
-        f[0] = make_float4(v[0], v[1], v[2], v[3]);
-        f[1] = make_float4(v[4], v[5], v[6], v[7]);
-    } else {
-        bf16x8_t o;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = (__bf16)v[i];
-        *reinterpret_cast<bf16x8_t*>(to) = o;
-    }
 }
 
 // A row behind a buffer descriptor (its base has to be the same for a wavefront): lanes behind the row's end read zeros and
