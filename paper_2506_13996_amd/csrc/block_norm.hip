@@ -3,7 +3,7 @@
 // A row is held in the registers of W wavefronts, 8 * VPT values a lane, so that everything is read and written once; its
 // sums (mean squares, and in backward the two products of a norm's gradient) go over the wavefronts through LDS.  Both are
 // bound by HBM: forward at 32768 x 4096 (norms before and after, 1.07 GB) 180 us = 6.0 TB/s, backward at 256000 x 4096 (12.6 GB)
-// 2.34 to 2.38 ms = 5.3 TB/s, of the 5.5 to 5.7 that a kernel reaches here that only reads four matrices and writes two.
+// 2.36 to 2.38 ms = 5.3 TB/s, of the 5.5 to 5.7 that a kernel reaches here that only reads four matrices and writes two.
 // Values stay packed bf16 in the registers between the passes over a row (stay_packed, made_here): with the conversions and
 // sums where the compiler puts them backward needs twice the registers and took 5.3 ms.
 #include <algorithm>
@@ -57,10 +57,11 @@ struct RowPlace {
     }
 };
 
-// sigmoid(z) and 1 - sigmoid(z), both to a few steps of fp32 however large |z| is: from t = exp(-|z|), whose exponent is
-// formed in two parts (v_exp_f32 is exact to a step, the product with log2 e is not), and 1 / (1 + t) by one step of Newton's
-// iteration, which gives the bits of the quotient or their neighbours at a third of its instructions.  32768 x 5120
-// backward with a gate for each element, otherwise as it was then: 1302 us with expf and the quotient, 1173 like this.
+// sigmoid(z) and 1 - sigmoid(z), both to a few steps of fp32, or to 2^-126 where one of them is below that (|z| > 87; v_exp_f32 need
+// not hold smaller results): from t = exp(-|z|), whose exponent is formed in two parts (v_exp_f32 is exact to a step, the product with
+// log2 e is not), and 1 / (1 + t) by one step of Newton's iteration, which gives the bits of the quotient or their neighbours at a
+// third of its instructions.  32768 x 5120 backward with a gate for each element, otherwise as it was then: 1302 us with expf and the
+// quotient, 1173 like this.
 struct Gate { float on, off; };
 __device__ __forceinline__ Gate gate_of(float z) {
     constexpr float kLog2e = 1.44269502e+00f, kLog2eRest = 1.92596299e-08f, kLn2 = 6.93147182e-01f;

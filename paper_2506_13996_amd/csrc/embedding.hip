@@ -446,7 +446,11 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Pair* __restri
 // host
 // ---------------------------------------------------------------------------------------------
 constexpr int kMostRun = 128;
-// zeros beside a pass of the sort that moves rows (12 us) and beside the joins (18 us): about what the memory takes in that time
+// Zeros beside a pass of the sort that moves rows (12 us) and beside the joins (18 us): about what the memory takes in that time, which
+// hardly goes by N and H.  Beside a pass, 64 MB against none / 32 / 128: 131072 x 4096 of 128256 434 us against 443 / 440 / 432, 8192 x
+// 8192 of 128256 446 against 460 / 450 / 440, 16384 x 1600 of 50257 57 against 65 / 59 / 65; narrow rows lose, 300000 x 256 of 200000 114
+// against 109 / 109 / 113.  Beside the joins, 96 MB against none / 48 / 192: the first 434 against 436 / 434 / 438, the second 446
+// against 448 / 446 / 443, the others the same.
 constexpr int64_t kZerosBesidePass = (int64_t)64 << 20, kZerosBesideJoins = (int64_t)96 << 20;
 constexpr int kShortBits = 12;                 // up to 4096 rows are sorted by one workgroup, beside zeros for every row (3001 x 1600 of
                                                // 50257: 42 us; 51 when the zeros wait for the marks of the sorted tokens)
