@@ -20,7 +20,7 @@
  *   dp   = s sigmoid(z) dr,  dz = s sigmoid'(z) p dr (summed over the row for a gate of one logit a row)
  *   db   = q1 (dp (w_post + o) - x1 mean(dp (w_post + o) x1))              dw_post = sum_rows dp x1
  *
- * All arithmetic is fp32 (a row whose sum of squares is beyond it, values of 1e18 and more, is normalised to zeros) and every
+ * All arithmetic is fp32 (a row whose sum of squares is beyond it, 4096 values of 3e17 or one of 2e19, is normalised to zeros) and every
  * output is rounded once; n is made from the r' before its rounding, the
  * gradients from the r' as it was stored.  Conventions are those of alst.h: device pointers, dense row-major
  * without strides, H a multiple of 8, 16-byte aligned base pointers, the caller owns every buffer, calls

@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from tests.test_gpu_block_norm import _inputs, _run_backward
+from tests.test_gpu_block_norm import _check_forward, _inputs, _run_backward, _run_forward
 
 pytestmark = pytest.mark.gpu
 
@@ -27,3 +27,21 @@ def test_a_branch_under_a_gate_alone_is_not_in_its_own_gradient(N, H, fp32, gate
                 assert torch.equal(got[k][same], want[k][same]) and not torch.isfinite(got[k][~same]).any()
             else:
                 assert torch.equal(got[k], want[k]), k
+
+
+@pytest.mark.parametrize("fp32", [False, True])
+def test_rows_whose_squares_fp32_cannot_add_up(fp32):
+    """4096 * 2.8e17^2 = 3.2e38 is below fp32's largest number 3.4e38 by more than the sum's roundings, 4096 * 3e17^2 = 3.7e38 and
+    (2e19)^2 = 4e38 are above it: such a row is normalised to zeros."""
+    N, H = 6, 4096
+    x = _inputs(N, H, True, "none", True, fp32)
+    x["r"][1], x["b"][1] = 2.8e17, 0
+    _check_forward(x, *_run_forward(x, fp32))
+    x["r"][2], x["b"][2] = 3e17, 0
+    x["r"][3], x["b"][3] = 0, 0
+    x["r"][3, 77] = -2e19
+    x["b"][4] = 3e17
+    ro, n = _run_forward(x, fp32)
+    assert torch.equal(ro[2:5].cpu(), x["r"][2:5]) and (n[2:4] == 0).all()
+    got = _run_backward(x, fp32)
+    assert torch.equal(got["d_residual"][2:4].cpu(), x["du"][2:4]) and (got["d_branch"][4] == 0).all()
